@@ -130,11 +130,11 @@ def prepare(case, seed):
     teacher = _rows(n, V, g, torch.float32)
     values, ids = teacher.topk(k, -1)
     ids = ids.int()
-    if case["skip"]:   # rows whose teacher had fewer than k entries
+    if case["skip"]:   # rows whose teacher has fewer than k entries, under a mask
         short = torch.rand(n, generator=g, device="cuda") < case["skip"]
         gone = short[:, None] & (torch.arange(k, device="cuda") >= (k + 1) // 2)
         values, ids = values.masked_fill(gone, -math.inf), ids.masked_fill(gone, -1)
-    lse = (teacher / case["T"]).logsumexp(-1)
+    lse = torch.where((ids < 0).any(-1), (values / case["T"]).logsumexp(-1), (teacher / case["T"]).logsumexp(-1))
     student = torch.empty_like(teacher).normal_(0.0, 1.2, generator=g).add_(teacher, alpha=0.8).to(_type(case))
     weights = torch.rand(n, generator=g, device="cuda") + 0.5
     weights[n - _padding(case):] = 0.0
@@ -230,7 +230,7 @@ def _plain_distill(s):
     t = (s["values"].double() / T).masked_fill(~valid, -math.inf)
     if case["tail"]:
         lp = t - s["lse"].double()[:, None]
-        lpr = (1.0 - lp.exp().sum(-1)).clamp(min=0.0).log()
+        lpr = (1.0 - lp.exp().sum(-1)).clamp(min=0.0).log().masked_fill(~valid.all(-1), -math.inf)   # a short record is all there is
     else:
         m = t.amax(-1, keepdim=True)
         lp = t - m - (t - m).exp().sum(-1, keepdim=True).log()
@@ -338,7 +338,7 @@ def _exact_distill(case, s):
         p = torch.zeros_like(z.detach())
         if case["tail"]:
             p[valid.nonzero()[:, 0], ids[valid]] = (t - s["lse"][part].double()[:, None]).exp()[valid]
-            left = (1.0 - p.sum(-1)).clamp(min=0.0)
+            left = (1.0 - p.sum(-1)).clamp(min=0.0) * valid.all(-1)
         else:
             p[valid.nonzero()[:, 0], ids[valid]] = t.masked_fill(~valid, -math.inf).softmax(-1)[valid]
             left = torch.zeros_like(w)
