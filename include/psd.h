@@ -311,6 +311,94 @@ int64_t psd_get_accept_expiries(void);
 int psd_sample(const float* logits, int32_t n_rows, int32_t vocab, float temperature, uint64_t seed,
                uint32_t position0, int32_t where, int32_t* tokens_out);
 
+/* ---- Rows of logits around the stages: adjusting, recording, distilling --------------------------------------
+ * Three operators on rows of logits.  All pointers are DEVICE memory of the current device; the calls only enqueue work on
+ * `stream` (a hipStream_t passed as void*, NULL = the default stream), allocate nothing and may be captured into a graph.
+ *   - dtype: PSD_F32 or PSD_BF16, the type of the logits (and of what is written in their shape); arithmetic is fp32 or wider and
+ *     rounded once.  Rows start `stride` elements apart (>= vocab) and need the alignment of one element only; what lies between
+ *     the end of a row and the next one is neither read nor written.  1 <= rows of a call <= 65535.
+ *   - Logits are finite or -inf; an entry of -inf has probability 0.
+ *   - A workspace belongs to one call until its kernels are done: calls (or captured graphs) that may overlap need one each.  Nothing in
+ *     it outlives the call.
+ *   - Results do not depend on scheduling: equal arguments give equal bits. */
+
+/* Adjusting: penalties for repeated tokens, biases and masks, for n_seqs sequences of `rows` logits rows each, as one verify
+ * pass leaves them: row (s, j), at index s * rows + j, belongs to the token that follows the history of sequence s and the first j
+ * tokens of its window.  ACCEPT compares like with like when the verifier's and the proposer's rows get the same window.
+ *   z1 = z > 0 ? z / repetition : z * repetition     where the token occurs in the history or the window's first j
+ *   z2 = z1 - (c * frequency + presence)              c > 0 occurrences, the first n_prompt tokens of the history not counted
+ *   z3 = z2 + bias                                    finite or -inf; of several entries for a token the last one counts
+ *   out = z3, or -inf where the row's mask has a 0 bit (whatever the logit was, a NaN among them)
+ * Every member may be NULL (none of that kind):
+ *   history          tokens of all sequences; sequence s has history_offsets[s] .. history_offsets[s + 1] - 1 (offsets: n_seqs + 1 of
+ *                    them; they are brought into 0 .. n_history, and an end before its beginning means none)
+ *   n_prompt         [n_seqs]
+ *   window           [n_seqs][window_stride], the first rows - 1 of each used; window_stride >= rows - 1
+ *   penalties        [n_seqs][3]: repetition, presence, frequency; a repetition that is not above 0 counts as 1
+ *   bias_tokens, bias  lists of all sequences, bias_offsets as history_offsets with n_bias
+ *   masks            [n_masks][(vocab + 31) / 32] words, bit v % 32 of word v / 32 set: token v is allowed (a grammar's states, say)
+ *   mask_index       [n_seqs * rows]: the mask of a row, -1 for none; for any other number outside 0 .. n_masks - 1 nothing is allowed
+ * Tokens outside 0 .. vocab - 1 (in history, window or bias_tokens) are passed over.  A row whose mask allows nothing comes out as -inf
+ * throughout and is no distribution: psd_top_logits reports no entry for it, and ACCEPT must not be given it.
+ * out may be `logits` itself (with equal strides); other overlaps are refused.
+ * Errors: PSD_EINVAL (null or misaligned pointers, sizes, strides, a list without its offsets, masks without mask_index, overlap), PSD_EHIP. */
+typedef struct {
+    const int32_t* history;
+    const int64_t* history_offsets;
+    int64_t n_history;
+    const int32_t* n_prompt;
+    const int32_t* window;
+    int64_t window_stride;
+    const float* penalties;
+    const int32_t* bias_tokens;
+    const float* bias;
+    const int64_t* bias_offsets;
+    int64_t n_bias;
+    const uint32_t* masks;
+    const int32_t* mask_index;
+    int64_t n_masks;
+} psd_adjust;
+int psd_adjust_logits(const void* logits, void* out, int32_t dtype, int32_t n_seqs, int32_t rows, int32_t vocab,
+                      int64_t logits_stride, int64_t out_stride, const psd_adjust* adjust, void* stream);
+
+/* Recording: the k largest entries of every row in descending order, equal ones in ascending order of their tokens, and
+ * ln sum_v exp(z_v / temperature): top log-probabilities (value / temperature - lse), or what psd_distill reads of a teacher.
+ *   values [n_rows][k] floats (the logits), ids [n_rows][k], lse [n_rows] (may be NULL)
+ * Where a row has fewer than k entries above -inf, the places behind them hold -inf and token -1 (lse of a row without any: -inf).
+ * 1 <= k <= PSD_MAX_TOP, k <= vocab.  workspace: psd_top_logits_workspace_bytes(n_rows, vocab, k) bytes, 16-byte aligned.
+ * Errors: PSD_EINVAL, PSD_ENOMEM (workspace too small), PSD_EHIP. */
+#define PSD_MAX_TOP 256
+size_t psd_top_logits_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t k);
+int psd_top_logits(const void* logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t stride, int32_t k,
+                   float temperature, float* values, int32_t* ids, float* lse, void* workspace, size_t workspace_bytes,
+                   void* stream);
+
+/* Distilling: the divergence between a teacher's record (psd_top_logits on the verifier's rows) and a student's rows (the
+ * proposer's), which is what acceptance depends on, and its gradient with respect to the student's logits z.
+ *   q = softmax(z / temperature);  S: the tokens of the row's record, which are k places of (value, token); a place whose token is
+ *   outside 0 .. vocab - 1, or stands in an earlier place of the row already, is passed over; a negative token also says that the
+ *   record is complete: the teacher has no entries beside it (a row under a grammar's mask, say)
+ *   p_i = exp(value_i / temperature - lse) with the record's lse (taken at the same temperature); without (top_lse NULL) the record
+ *   is the whole teacher: p = softmax of its values / temperature
+ *   Outcomes: the tokens of S, and one more for all others together: p_rest = max(0, 1 - sum p_i), or 0 where the record is
+ *   complete or S the whole vocabulary; q_rest = the student's mass outside S.
+ *   PSD_DIV_KL   sum p ln(p / q)          PSD_DIV_JSD   Div of this library on these outcomes: never above Div of the whole rows
+ *   loss[r] = row_weights[r] * divergence,  grad[r][v] = d loss[r] / d z[r][v]
+ * row_weights NULL: 1 everywhere.  A row of weight 0 (padding), or without a valid place, has loss 0 and gradient 0; its student row
+ * is not looked at.  KL is +inf where the student has no mass for an outcome of the teacher; a student row without any entry above -inf has loss
+ * NaN.  row_weights is also where a gradient with respect to the losses goes: a second call then yields the product.
+ *   top_values, top_ids [n_rows][k], 1 <= k <= PSD_MAX_TOP; top_lse, row_weights, loss [n_rows]
+ *   grad: rows as the logits', of their type, grad_stride apart; NULL: the loss alone.  It may be `logits` itself (with equal
+ *   strides); other overlaps are refused.
+ *   workspace: psd_distill_workspace_bytes(n_rows, vocab, k) bytes, 16-byte aligned
+ * Errors: PSD_EINVAL, PSD_ENOMEM (workspace too small), PSD_EHIP. */
+enum { PSD_DIV_KL = 0, PSD_DIV_JSD = 1 };
+size_t psd_distill_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t k);
+int psd_distill(const void* logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t stride, const float* top_values,
+                const int32_t* top_ids, const float* top_lse, int32_t k, float temperature, int32_t divergence,
+                const float* row_weights, float* loss, void* grad, int64_t grad_stride, void* workspace,
+                size_t workspace_bytes, void* stream);
+
 /* Test hook: the device's Philox4x32-10, the generator behind every draw above, for the n consecutive counters
  * (c0 .. c0 + n - 1, c1, c2, c3) under key = seed.  out [n][4] uint32 raw words and / or u_out [n][4] floats (the
  * uniforms the kernels derive from them: (top 23 bits + 1/2) / 2^23); either may be NULL.  where: 0 host pointers,

@@ -92,6 +92,11 @@ def lib():
         L.orc_generate.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(Params), C.c_void_p, C.c_int,
                                    C.c_int, C.c_uint64, C.c_void_p, C.POINTER(Stats)]
         L.orc_row_stats.argtypes = [C.c_void_p, C.c_int, C.c_double, C.c_void_p, C.c_void_p]
+        L.orc_adjust_row.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int, C.c_double, C.c_double,
+                                     C.c_double, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_void_p]
+        L.orc_top_row.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_double, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.orc_distill_row.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_double, C.c_int, C.c_double,
+                                      C.c_void_p, C.c_void_p]
         L.orc_accept_assisted.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_double, C.c_uint64, C.c_uint32,
                                           C.c_uint32, C.c_int, C.c_void_p]
         L.orc_generate_assisted.restype = C.c_int
@@ -216,6 +221,37 @@ def row_stats(logits, temperature=1.0):
     h, m = C.c_double(0), C.c_double(0)
     lib().orc_row_stats(lg.ctypes.data, lg.size, temperature, C.byref(h), C.byref(m))
     return h.value, m.value
+
+
+def adjust_row(z, history=(), n_prompt=0, window=(), penalties=(1.0, 0.0, 0.0), bias_tokens=(), bias=(), mask=None, closed=False):
+    """One row of logits adjusted: penalties (repetition, presence, frequency) for history and window, biases, mask words."""
+    z = np.ascontiguousarray(z, dtype=np.float32)
+    h, w, bt = (np.ascontiguousarray(a, dtype=np.int32) for a in (history, window, bias_tokens))
+    b = np.ascontiguousarray(bias, dtype=np.float32)
+    m = None if mask is None else np.ascontiguousarray(mask, dtype=np.uint32)
+    out = np.empty(z.size, dtype=np.float64)
+    lib().orc_adjust_row(z.ctypes.data, z.size, h.ctypes.data, h.size, n_prompt, w.ctypes.data, w.size, *(float(x) for x in penalties),
+                         bt.ctypes.data, b.ctypes.data, b.size, None if m is None else m.ctypes.data, int(closed), out.ctypes.data)
+    return out
+
+
+def top_row(z, k, temperature=1.0):
+    """(values [k], ids [k], lse) of one row: its k largest entries, equal ones by ascending token, and ln sum exp(z / temperature)."""
+    z = np.ascontiguousarray(z, dtype=np.float32)
+    values, ids, lse = np.empty(k, np.float64), np.empty(k, np.int32), np.empty(1, np.float64)
+    lib().orc_top_row(z.ctypes.data, z.size, k, temperature, values.ctypes.data, ids.ctypes.data, lse.ctypes.data)
+    return values, ids, lse[0]
+
+
+def distill_row(z, values, ids, lse, temperature=1.0, divergence=0, weight=1.0, want_grad=True):
+    """(loss, grad [vocab]) of one student row against a record; lse None: the record is the whole teacher."""
+    z, values = (np.ascontiguousarray(a, dtype=np.float32) for a in (z, values))
+    ids = np.ascontiguousarray(ids, dtype=np.int32)
+    ls = None if lse is None else np.array([lse], dtype=np.float32)
+    loss, grad = np.empty(1, np.float64), np.empty(z.size, np.float64)
+    lib().orc_distill_row(z.ctypes.data, z.size, values.ctypes.data, ids.ctypes.data, None if ls is None else ls.ctypes.data, ids.size,
+                          temperature, divergence, weight, loss.ctypes.data, grad.ctypes.data if want_grad else None)
+    return loss[0], grad
 
 
 def accept_assisted(logits_p, x, temperature=1.0, seed=0, position0=0, stage=1, take_bonus=True):

@@ -150,6 +150,126 @@ void orc_row_stats(const float* logits, int V, double temperature, double* entro
 }
 
 /* ------------------------------------------------------------------------- */
+/* Rows of logits around the stages: adjusting, recording, distilling        */
+/* ------------------------------------------------------------------------- */
+
+/* One row: penalties for the tokens of the history (its first n_prompt ones count for repetition only) and of the n_window tokens after
+ * it, biases (the last entry of a token), mask bits (NULL: none; closed: nothing is allowed). */
+void orc_adjust_row(const float* z, int V, const int32_t* history, int64_t n_history, int64_t n_prompt, const int32_t* window,
+                    int n_window, double repetition, double presence, double frequency, const int32_t* bias_tokens, const float* bias,
+                    int64_t n_bias, const uint32_t* mask, int closed, double* out) {
+    int64_t* seen = (int64_t*)calloc((size_t)V, sizeof(int64_t));
+    int64_t* count = (int64_t*)calloc((size_t)V, sizeof(int64_t));
+    double* add = (double*)calloc((size_t)V, sizeof(double));
+    for (int64_t i = 0; i < n_history; ++i)
+        if (history[i] >= 0 && history[i] < V) {
+            ++seen[history[i]];
+            if (i >= n_prompt) ++count[history[i]];
+        }
+    for (int i = 0; i < n_window; ++i)
+        if (window[i] >= 0 && window[i] < V) {
+            ++seen[window[i]];
+            ++count[window[i]];
+        }
+    for (int64_t i = 0; i < n_bias; ++i)
+        if (bias_tokens[i] >= 0 && bias_tokens[i] < V) add[bias_tokens[i]] = bias[i];
+    if (!(repetition > 0.0)) repetition = 1.0;
+    for (int v = 0; v < V; ++v) {
+        double y = z[v];
+        if (seen[v]) y = y > 0.0 ? y / repetition : y * repetition;
+        if (count[v]) y -= (double)count[v] * frequency + presence;
+        y += add[v];
+        if (closed || (mask && !((mask[v >> 5] >> (v & 31)) & 1u))) y = -INFINITY;
+        out[v] = y;
+    }
+    free(seen);
+    free(count);
+    free(add);
+}
+
+/* ln sum exp(z / T) over the entries for which skip (may be NULL) is 0; -inf where there is none */
+static double log_sum(const float* z, int V, double T, const unsigned char* skip) {
+    double m = -INFINITY, s = 0.0;
+    for (int v = 0; v < V; ++v)
+        if (!(skip && skip[v]) && z[v] / T > m) m = z[v] / T;
+    if (m == -INFINITY) return m;
+    for (int v = 0; v < V; ++v)
+        if (!(skip && skip[v])) s += exp(z[v] / T - m);
+    return m + log(s);
+}
+
+/* The k largest entries above -inf, descending, equal ones by ascending token; (-inf, -1) in places without one. */
+void orc_top_row(const float* z, int V, int k, double T, double* values, int32_t* ids, double* lse) {
+    unsigned char* used = (unsigned char*)calloc((size_t)V, 1);
+    for (int i = 0; i < k; ++i) {
+        int best = -1;
+        for (int v = 0; v < V; ++v)
+            if (!used[v] && z[v] > -INFINITY && (best < 0 || z[v] > z[best])) best = v;
+        values[i] = best < 0 ? -INFINITY : z[best];
+        ids[i] = best;
+        if (best >= 0) used[best] = 1;
+    }
+    *lse = log_sum(z, V, T, NULL);
+    free(used);
+}
+
+/* Divergence of one student row from a record, and its gradient (may be NULL).  divergence: 0 KL, 1 Jensen-Shannon.  From the
+ * definition: probabilities of the K + 1 outcomes, dl/dq of each, then the softmax's derivative. */
+void orc_distill_row(const float* z, int V, const float* values, const int32_t* ids, const float* lse, int k, double T, int divergence,
+                     double weight, double* loss, double* grad) {
+    unsigned char* in_s = (unsigned char*)calloc((size_t)V, 1);
+    int* tok = (int*)malloc((size_t)k * sizeof(int));
+    double* p = (double*)malloc((size_t)(k + 1) * sizeof(double));
+    double* w = (double*)malloc((size_t)(k + 1) * sizeof(double));    /* q_b dl/dq_b */
+    int n = 0, complete = 0;
+    double m = -INFINITY, total = 0.0;
+    for (int i = 0; i < k; ++i) {
+        if (ids[i] < 0) complete = 1;
+        if (ids[i] < 0 || ids[i] >= V || in_s[ids[i]]) continue;
+        in_s[ids[i]] = 1;
+        tok[n] = ids[i];
+        p[n++] = values[i] / T;
+        if (values[i] / T > m) m = values[i] / T;
+    }
+    *loss = 0.0;
+    if (grad) for (int v = 0; v < V; ++v) grad[v] = 0.0;
+    if (n == 0 || weight == 0.0) {
+        free(in_s); free(tok); free(p); free(w);
+        return;
+    }
+    for (int i = 0; i < n; ++i) total += p[i] = exp(p[i] - (lse ? (double)*lse : m));
+    p[n] = 0.0;
+    if (lse) p[n] = complete || n == V || total >= 1.0 ? 0.0 : 1.0 - total;
+    else for (int i = 0; i < n; ++i) p[i] /= total;
+    const double all = log_sum(z, V, T, NULL), rest = log_sum(z, V, T, in_s);
+    double l = 0.0, sum_w = 0.0;
+    for (int i = 0; i <= n; ++i) {
+        const double lq = (i < n ? z[tok[i]] / T : rest) - all, q = exp(lq);
+        if (divergence == 0) {
+            if (p[i] > 0.0) l += p[i] * (log(p[i]) - lq);
+            w[i] = -p[i];
+        } else {
+            const double mid = 0.5 * (p[i] + q);
+            if (p[i] > 0.0) l += 0.5 * p[i] * log(p[i] / mid);
+            if (q > 0.0) l += 0.5 * q * log(q / mid);
+            w[i] = q > 0.0 ? 0.5 * q * log(q / mid) : 0.0;
+        }
+        sum_w += w[i];
+    }
+    *loss = all == -INFINITY ? NAN : weight * l;
+    if (grad) {
+        /* within the others the derivative spreads by their own distribution */
+        for (int v = 0; v < V; ++v)
+            if (!in_s[v]) {
+                const double share = z[v] > -INFINITY ? exp(z[v] / T - rest) : 0.0;
+                grad[v] = weight / T * share * (w[n] - exp(rest - all) * sum_w);
+            }
+        for (int i = 0; i < n; ++i) grad[tok[i]] = weight / T * (w[i] - exp(z[tok[i]] / T - all) * sum_w);
+    }
+    free(in_s); free(tok); free(p); free(w);
+}
+
+/* ------------------------------------------------------------------------- */
 /* ACCEPT: one verify stage over k proposed tokens                           */
 /* ------------------------------------------------------------------------- */
 

@@ -14,6 +14,8 @@ FLAG_ASSISTED = 2
 FLAG_ROW_STATS = 4
 FLAG_GREEDY = 8
 MAX_WIDTH = 32
+MAX_TOP = 256
+DIV_KL, DIV_JSD = 0, 1
 
 
 class PsdError(RuntimeError):
@@ -54,6 +56,22 @@ class Adapt(C.Structure):
                 ("T_t_max", C.c_float)]
 
 
+class Adjust(C.Structure):
+    """psd_adjust: what psd_adjust_logits does to the rows.  Takes device buffers (objects with data_ptr()) or None and holds on to
+    them; n_history, n_bias and n_masks are the numbers of tokens, biases and masks in them."""
+    _fields_ = [("history", C.c_void_p), ("history_offsets", C.c_void_p), ("n_history", C.c_int64), ("n_prompt", C.c_void_p),
+                ("window", C.c_void_p), ("window_stride", C.c_int64), ("penalties", C.c_void_p), ("bias_tokens", C.c_void_p),
+                ("bias", C.c_void_p), ("bias_offsets", C.c_void_p), ("n_bias", C.c_int64), ("masks", C.c_void_p),
+                ("mask_index", C.c_void_p), ("n_masks", C.c_int64)]
+
+    def __init__(self, history=None, history_offsets=None, n_history=0, n_prompt=None, window=None, window_stride=0, penalties=None,
+                 bias_tokens=None, bias=None, bias_offsets=None, n_bias=0, masks=None, mask_index=None, n_masks=0):
+        self._buffers = (history, history_offsets, n_prompt, window, penalties, bias_tokens, bias, bias_offsets, masks, mask_index)
+        super().__init__(_dev_ptr(history), _dev_ptr(history_offsets), n_history, _dev_ptr(n_prompt), _dev_ptr(window), window_stride,
+                         _dev_ptr(penalties), _dev_ptr(bias_tokens), _dev_ptr(bias), _dev_ptr(bias_offsets), n_bias, _dev_ptr(masks),
+                         _dev_ptr(mask_index), n_masks)
+
+
 class KernelStat(C.Structure):
     _fields_ = [("name", C.c_char * 48), ("launches", C.c_int64), ("ms_total", C.c_double), ("bytes_total", C.c_double)]
 
@@ -88,6 +106,17 @@ def lib():
         L.psd_accept_batch_noalloc.argtypes = L.psd_accept_batch.argtypes[:15] + [C.c_void_p]
         L.psd_philox_block.argtypes = [C.c_uint64, C.c_uint32, C.c_uint32, C.c_uint32, C.c_uint32, C.c_uint32, C.c_int32,
                                        C.c_void_p, C.c_void_p]
+        L.psd_adjust_logits.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int64,
+                                        C.POINTER(Adjust), C.c_void_p]
+        L.psd_top_logits_workspace_bytes.restype = C.c_size_t
+        L.psd_top_logits_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
+        L.psd_top_logits.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.c_float, C.c_void_p,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.psd_distill_workspace_bytes.restype = C.c_size_t
+        L.psd_distill_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
+        L.psd_distill.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
+                                  C.c_float, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t,
+                                  C.c_void_p]
         L.psd_sample.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_float, C.c_uint64, C.c_uint32, C.c_int32,
                                  C.c_void_p]
         L.psd_dev_alloc.argtypes = [C.c_size_t, C.POINTER(C.c_void_p)]
@@ -138,6 +167,15 @@ def _ptr(a):
     if isinstance(a, np.ndarray):
         return a.ctypes.data
     return a.data_ptr()
+
+
+def _dev_ptr(a):
+    """Address of a device buffer; host arrays are refused (a kernel must not be given their addresses)."""
+    if a is None:
+        return None
+    if not hasattr(a, "data_ptr"):
+        raise TypeError(f"a device buffer (an object with data_ptr()) is needed, not {type(a).__name__}")
+    return a.data_ptr() or None
 
 
 class DeviceBuffer:
@@ -262,6 +300,35 @@ def accept_batch_noalloc(logits_p, logits_q, tokens, n_trials, k, vocab, T, temp
     _check(lib().psd_accept_batch_noalloc(_ptr(logits_p), _ptr(logits_q), _ptr(tokens), n_trials, k, vocab, T,
                                           temperature, seed, position0, stage, int(take_bonus), _ptr(n_accepted),
                                           _ptr(next_token), _ptr(div_out), stream))
+
+
+def adjust_logits(logits, out, n_seqs, rows, vocab, adjust, dtype=F32, logits_stride=None, out_stride=None, stream=None):
+    """psd_adjust_logits on device buffers: n_seqs * rows rows of `vocab` logits (strides default to vocab); only enqueues."""
+    _check(lib().psd_adjust_logits(_dev_ptr(logits), _dev_ptr(out), dtype, n_seqs, rows, vocab,
+                                   vocab if logits_stride is None else logits_stride, vocab if out_stride is None else out_stride,
+                                   C.byref(adjust), stream))
+
+
+def top_logits_workspace_bytes(n_rows, vocab, k):
+    return lib().psd_top_logits_workspace_bytes(n_rows, vocab, k)
+
+
+def top_logits(logits, n_rows, vocab, k, temperature, values, ids, lse, workspace, workspace_bytes, dtype=F32, stride=None, stream=None):
+    """psd_top_logits on device buffers: values [n_rows, k] floats, ids [n_rows, k] int32, lse [n_rows] floats or None; only enqueues."""
+    _check(lib().psd_top_logits(_dev_ptr(logits), dtype, n_rows, vocab, vocab if stride is None else stride, k, temperature,
+                                _dev_ptr(values), _dev_ptr(ids), _dev_ptr(lse), _dev_ptr(workspace), workspace_bytes, stream))
+
+
+def distill_workspace_bytes(n_rows, vocab, k):
+    return lib().psd_distill_workspace_bytes(n_rows, vocab, k)
+
+
+def distill(logits, n_rows, vocab, top_values, top_ids, top_lse, k, temperature, divergence, row_weights, loss, grad, workspace,
+            workspace_bytes, dtype=F32, stride=None, grad_stride=None, stream=None):
+    """psd_distill on device buffers: loss [n_rows] floats, grad rows like the logits' or None (the loss alone); only enqueues."""
+    _check(lib().psd_distill(_dev_ptr(logits), dtype, n_rows, vocab, vocab if stride is None else stride, _dev_ptr(top_values),
+                             _dev_ptr(top_ids), _dev_ptr(top_lse), k, temperature, divergence, _dev_ptr(row_weights), _dev_ptr(loss),
+                             _dev_ptr(grad), vocab if grad_stride is None else grad_stride, _dev_ptr(workspace), workspace_bytes, stream))
 
 
 def sample_device(logits, n_rows, vocab, temperature, seed, position0, tokens_out):

@@ -48,7 +48,6 @@ constexpr int kAccThreads = 256;
 constexpr int kQuadsPerThread = kAcceptChunk / 4 / kAccThreads;  // 2 (sampling and race kernels)
 constexpr int kSweepQuads = 5, kSweepChunk = kSweepQuads * 4 * kAccThreads, kSweepWaves = kAccThreads / 64;
 constexpr int kSweepMaxSlots = 256;    // per-wave results of a row that workgroups wait for in the one-launch sweep
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 constexpr float kBig = 1e30f;
 constexpr unsigned long long kWaitTicks = 5000000ull;  // 50 ms of the 100 MHz wall clock
 constexpr uint32_t kUnwritten = 0xffffffffu;           // a NaN pattern no maximum can have
@@ -92,41 +91,6 @@ __device__ inline void load4_stream(const float* row, int v, int V, bool vec, fl
 #pragma unroll
         for (int e = 0; e < 4; ++e) out[e] = (v + e < V) ? row[v + e] : -INFINITY;
     }
-}
-
-__device__ inline float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ inline float fast_log2(float x) { return __builtin_amdgcn_logf(x); }
-
-// ---- wave reductions on the data-parallel-primitive lanes (no LDS traffic) ----------------------
-// xor 1, xor 2, mirror within 8, mirror within 16: every lane of a row of 16 then holds the row's
-// result; two row broadcasts carry it to the last row, whose lane 63 is read out.  Fixed shape, so a
-// sum has fixed rounding.  Results are wave-uniform.
-template <int CTRL, int ROW_MASK, bool BOUND>
-__device__ inline float dpp_move(float old, float v) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(v), CTRL, ROW_MASK, 0xf, BOUND));
-}
-__device__ inline float wave_sum_dpp(float v) {
-    v = v + dpp_move<0xB1, 0xf, true>(0.f, v);    // quad_perm [1,0,3,2]
-    v = v + dpp_move<0x4E, 0xf, true>(0.f, v);    // quad_perm [2,3,0,1]
-    v = v + dpp_move<0x141, 0xf, true>(0.f, v);   // row_half_mirror
-    v = v + dpp_move<0x140, 0xf, true>(0.f, v);   // row_mirror
-    v = v + dpp_move<0x142, 0xa, false>(0.f, v);  // row_bcast15 into rows 1 and 3
-    v = v + dpp_move<0x143, 0xc, false>(0.f, v);  // row_bcast31 into rows 2 and 3
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
-}
-// the same shape for the maximum; written as instructions because the generic maximum would re-quiet
-// both operands at every step (s_nop 1: a lane-crossing read must not follow the write of its source directly)
-__device__ inline float wave_max_dpp(float v) {
-    asm volatile(
-        "s_nop 1\n\tv_max_f32_dpp %0, %0, %0 quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf bound_ctrl:1\n\t"
-        "s_nop 1\n\tv_max_f32_dpp %0, %0, %0 quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf bound_ctrl:1\n\t"
-        "s_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_half_mirror row_mask:0xf bank_mask:0xf bound_ctrl:1\n\t"
-        "s_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_mirror row_mask:0xf bank_mask:0xf bound_ctrl:1\n\t"
-        "s_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_bcast:15 row_mask:0xa bank_mask:0xf\n\t"
-        "s_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_bcast:31 row_mask:0xc bank_mask:0xf\n\t"
-        "s_nop 1"
-        : "+v"(v));
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
 struct RowStats { float Mp, Sp, Mq, Sq; };  // base 2: p_v = 2^(z_v c2 - Mp) / Sp
@@ -824,7 +788,6 @@ __global__ __launch_bounds__(64) void accept_pick(AcceptShape s, AcceptWs w, int
     if (threadIdx.x == 0) put_token(out, tok_out, b, tok);
 }
 
-static inline size_t align16(size_t n) { return (n + 15) & ~(size_t)15; }
 
 static int sweep_chunks(int vocab) { return (vocab + kSweepChunk - 1) / kSweepChunk; }
 

@@ -28,6 +28,8 @@ void set_error(char* dst, const char* fmt, ...);
         return (code);                             \
     } while (0)
 
+inline size_t align16(size_t n) { return (n + 15) & ~(size_t)15; }
+
 // ---- ACCEPT stage, device-level entry used by the scheduler and by the C ABI -------------------
 struct AcceptOut {   // one per trial, device memory
     int32_t n_accepted;
