@@ -48,7 +48,7 @@ struct Row<true> {
     }
 };
 
-// elements v .. v + N - 1 of a row of V; those at or beyond V read as -inf
+// elements v .. v + N - 1 of a row of V > v; those at or beyond V read as -inf
 template <bool BF16>
 __device__ inline raw16 row_load(const void* row, int v, int V) {
     typedef Row<BF16> R;
@@ -56,7 +56,9 @@ __device__ inline raw16 row_load(const void* row, int v, int V) {
     if (v + R::N <= V) return __builtin_nontemporal_load((const typename R::V*)p);
     float e[R::N];
 #pragma unroll
-    for (int i = 0; i < R::N; ++i) e[i] = v + i < V ? R::one(p + i) : -INFINITY;
+    for (int i = 0; i < R::N; ++i) e[i] = R::one(p + min(i, V - 1 - v));   // loads that need not wait for each other (v < V)
+#pragma unroll
+    for (int i = 0; i < R::N; ++i) e[i] = v + i < V ? e[i] : -INFINITY;
     return R::pack(e);
 }
 template <bool BF16>

@@ -436,6 +436,35 @@ def test_distill_odd_records_and_rows(dtype, div, reps):
     check_distill(z, values, ids, lse, T, div, weights, loss[:8], grad[:8], dtype)
 
 
+# enough bytes for every way a call can go: rows that pass by workgroups of three sizes, rows that are held by three sizes, chunks; a few
+# rows over and over, so that all but the first few need only be the same
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,row_bytes,odd,k", [
+    (257, 30 << 10, 1, 20), (300, 100 << 10, 3, 255), (300, 60 << 10, 0, 256), (2600, 100 << 10, 2, 64), (1300, 200 << 10, 1, 255), (1300, 200 << 10, 0, 256),
+    (560, 500 << 10, 3, 100), (40, 300 << 10, 1, 256), (300, 900 << 10, 2, 30), (5, 1100 << 10, 1, 256),
+])
+def test_distill_every_way(dtype, n, row_bytes, odd, k):
+    rng = np.random.default_rng(k)
+    V = row_bytes // (4 if dtype == psd.F32 else 2) - odd
+    few = 5
+    t, z = pair(rng, few, V, dtype)
+    values, ids, lse = records(t, k, 1.0)
+    ids[1, :12] = (np.arange(12) // 3 * 2 + V - 12) % V      # neighbours and repetitions, up to the row's end
+    z[2, ids[2]] = -40.0
+    z = rounded(z, dtype)
+    weights = np.array([1.0, 0.7, 2.0, 0.0, 1.5], np.float32)
+    at = np.arange(n) % few
+    x = Rows(z[at], dtype)
+    for div in (psd.DIV_KL, psd.DIV_JSD):
+        loss, grad = run_distill(x, n, V, values[at], ids[at], lse[at], k, 1.0, div, weights[at], dtype)
+        check_distill(z, values, ids, lse, 1.0, div, weights, loss[:few], grad[:few], dtype)
+        assert np.array_equal(loss, loss[at]) and all(np.array_equal(grad[i], grad[i % few]) for i in range(n))
+        only, _ = run_distill(x, n, V, values[at], ids[at], lse[at], k, 1.0, div, weights[at], dtype, want_grad=False)
+        assert np.array_equal(only, loss)
+    inside, gi = run_distill(x, n, V, values[at], ids[at], lse[at], k, 1.0, psd.DIV_JSD, weights[at], dtype, in_place=True)
+    assert np.array_equal(inside, loss) and np.array_equal(gi, grad)
+
+
 def test_distill_without_student_mass():
     V = 5000
     z = np.zeros((4, V), np.float32)
