@@ -241,26 +241,6 @@ __device__ inline float2 wave_join(float2 p, float c2) {
     return make_float2(m, wave_sum_dpp(p.y * fast_exp2((p.x - m) * c2)));
 }
 
-template <bool BF16>
-struct None;   // 16 bytes of -inf
-template <> struct None<false> { static constexpr uint32_t word = 0xff800000u; };
-template <> struct None<true> { static constexpr uint32_t word = 0xff80ff80u; };
-template <bool BF16>
-__device__ inline raw16 none16() { return raw16{None<BF16>::word, None<BF16>::word, None<BF16>::word, None<BF16>::word}; }
-
-template <bool BF16>
-__device__ inline float vec_max(const raw16& r, float m) {
-#pragma unroll
-    for (int x = 0; x < Row<BF16>::N; ++x) m = fmaxf(m, Row<BF16>::get(r, x));
-    return m;
-}
-template <bool BF16>
-__device__ inline float vec_sum(const raw16& r, float m, float c2, float s) {
-#pragma unroll
-    for (int x = 0; x < Row<BF16>::N; ++x) s += fast_exp2((Row<BF16>::get(r, x) - m) * c2);
-    return s;
-}
-
 // a vector with -inf in the places of the clear bits
 template <bool BF16>
 __device__ inline raw16 vec_only(const raw16& r, uint32_t on) {

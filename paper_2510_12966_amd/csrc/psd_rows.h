@@ -74,6 +74,26 @@ __device__ inline void row_store(void* row, int v, int V, const float* e) {
         if (v + i < V) R::put_one(p + i, e[i]);
 }
 
+template <bool BF16>
+struct None;   // 16 bytes of -inf
+template <> struct None<false> { static constexpr uint32_t word = 0xff800000u; };
+template <> struct None<true> { static constexpr uint32_t word = 0xff80ff80u; };
+template <bool BF16>
+__device__ inline raw16 none16() { return raw16{None<BF16>::word, None<BF16>::word, None<BF16>::word, None<BF16>::word}; }
+
+template <bool BF16>
+__device__ inline float vec_max(const raw16& r, float m) {
+#pragma unroll
+    for (int x = 0; x < Row<BF16>::N; ++x) m = fmaxf(m, Row<BF16>::get(r, x));
+    return m;
+}
+template <bool BF16>
+__device__ inline float vec_sum(const raw16& r, float m, float c2, float s) {
+#pragma unroll
+    for (int x = 0; x < Row<BF16>::N; ++x) s += fast_exp2((Row<BF16>::get(r, x) - m) * c2);
+    return s;
+}
+
 inline int row_elem(int dtype) { return dtype == PSD_BF16 ? 2 : 4; }
 
 // Two sets of rows are the same rows, or have no byte in common

@@ -1,10 +1,12 @@
 // The k largest entries of every row of logits, with the row's log-sum-exp.
 //
-// A workgroup streams over a segment of a row, 4096 entries at a time, and keeps a list of candidates in LDS: entries not below a
-// threshold that at least k entries of the segment are known to reach.  The first threshold is the k-th largest of the threads' own maxima in the
-// first block; whenever the list is cut to its k largest, their smallest becomes the threshold, and later entries have to exceed it (an equal
-// one has a higher token and comes behind).  Cuts are exact: radix selection, 8 bits a round, over 64-bit items (order-preserving image of
-// the value, complement of the token), which all differ, so that equal values fall in the order of their tokens by themselves.
+// A workgroup streams over a segment of a row, 4096 entries at a time with the next ones on their way, and keeps a list of candidates in LDS:
+// entries not below a threshold that at least k entries of the segment are known to reach.  The first threshold is the k-th largest of the
+// threads' own maxima in the first block; whenever the list is cut to its k largest (after 1, 2, 4 ... blocks), their smallest becomes the
+// threshold, and later entries have to exceed it (an equal one has a higher token and comes behind).  So all but a few hundred entries of a
+// row cost a maximum, an exponential and their load.  Items are 64 bits (order-preserving image of the value, complement of the token)
+// and all differ, so that equal values fall in the order of their tokens by themselves.  A cut drops what is below the k-th largest of the
+// threads' maxima once more and ranks the rest by comparing all pairs, or, where more than 256 are left, by radix selection, 8 bits a round.
 // Many rows: one segment each, one launch.  Few rows: several segments, whose lists a second launch merges.
 // Bound: the bytes of the rows, read once.
 #include "psd_rows.h"
@@ -14,9 +16,10 @@ namespace psd {
 constexpr int kTopThreads = 256;
 constexpr int kTopBlock = 4096;                       // entries between two looks at the list
 constexpr int kTopPer = kTopBlock / kTopThreads;      // of one thread: 16
-constexpr int kTopLow = 512;                          // a list longer than this is cut before the next block
+constexpr int kTopLow = 256;                          // a list longer than this is cut before the next block
 constexpr int kTopList = kTopLow + kTopBlock;         // so every entry of a block finds a place in it
-constexpr int kTopItems = kTopList / kTopThreads;     // 18
+constexpr int kTopItems = kTopList / kTopThreads;     // 17
+static_assert(PSD_MAX_TOP <= kTopThreads && PSD_MAX_TOP <= kTopLow, "a thread, and a place in a cut list, per entry of the result");
 
 typedef unsigned long long u64;
 
@@ -29,20 +32,53 @@ __device__ inline float value_of(uint32_t r) { return __uint_as_float(r & 0x8000
 __device__ inline u64 item_of(float z, int v) { return (u64)rank_of(z) << 32 | (uint32_t)~v; }
 
 struct TopLds {
-    u64 list[kTopList];
+    alignas(16) u64 list[kTopList];
     uint32_t hist[3][256];   // one is filled, the next cleared, the last may still be read
-    uint32_t maxima[kTopThreads];
+    alignas(16) uint32_t maxima[kTopThreads];
     float2 part[kTopThreads / 64];
+    uint32_t least[kTopThreads / 64];
+    u64 smallest[kTopThreads / 64];
     int count;
-    uint32_t least;
 };
 
-// Cuts a list of n items (k < n <= kTopList) to its k largest; returns the smallest of them.  All threads, n uniform.
-__device__ inline u64 cut_to(TopLds& l, int n, int k) {
+// over a wave, every lane gets it
+template <int CTRL>
+__device__ inline uint32_t max_moved(uint32_t v) { return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true)); }
+__device__ inline uint32_t wave_max_u32(uint32_t v) {
+    v = max_moved<0xB1>(v);    // quad_perm [1,0,3,2]
+    v = max_moved<0x4E>(v);    // quad_perm [2,3,0,1]
+    v = max_moved<0x141>(v);   // row_half_mirror
+    v = max_moved<0x140>(v);   // row_mirror
+    {
+        const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = max(p[0], p[1]);
+    }
+    const auto p = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return max(p[0], p[1]);
+}
+
+// The k-th largest of the threads' maxima (images, 0: no entry), so at least k items reach it; 1 where fewer than k threads have one.
+// All threads; two barriers.
+__device__ inline uint32_t kth_maximum(TopLds& l, uint32_t mine, int k) {
+    const int t = threadIdx.x;
+    l.maxima[t] = mine;
+    const int have = __syncthreads_count(mine != 0);
+    if (have < k) return 1;   // uniform
+    int above = 0;
+#pragma unroll 8
+    for (int i = 0; i < kTopThreads; i += 4) {
+        const uint4 o = *reinterpret_cast<const uint4*>(&l.maxima[i]);
+        above += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+    }
+    const uint32_t least = ~wave_max_u32(mine != 0 && above < k ? ~mine : 0u);
+    if ((t & 63) == 0) l.least[t >> 6] = least;
+    __syncthreads();
+    return min(min(l.least[0], l.least[1]), min(l.least[2], l.least[3]));
+}
+
+// Radix selection among the items it[] of all threads, of which more than k are not 0: the smallest of the k largest.  All threads.
+__device__ inline u64 kth_item(TopLds& l, const u64 (&it)[kTopItems], int k) {
     const int t = threadIdx.x, lane = t & 63;
-    u64 it[kTopItems];
-#pragma unroll
-    for (int i = 0; i < kTopItems; ++i) it[i] = t + kTopThreads * i < n ? l.list[t + kTopThreads * i] : 0;
     l.hist[0][t] = 0;
     __syncthreads();
     u64 least = 0;
@@ -78,37 +114,66 @@ __device__ inline u64 cut_to(TopLds& l, int n, int k) {
         least |= (u64)bin << shift;
         if ((uint32_t)need == size) break;   // the whole bin belongs to them
     }
-    if (t == 0) l.count = 0;
-    __syncthreads();
-    u64 mine = ~0ull;
-#pragma unroll
-    for (int i = 0; i < kTopItems; ++i)
-        if (it[i] != 0 && it[i] >= least) {
-            l.list[atomicAdd(&l.count, 1)] = it[i];
-            mine = min(mine, it[i]);
-        }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) mine = min(mine, (u64)__shfl_xor((long long)mine, d));
-    u64* smallest = reinterpret_cast<u64*>(l.maxima);
-    if (lane == 0) smallest[t >> 6] = mine;
-    __syncthreads();
-    return min(min(smallest[0], smallest[1]), min(smallest[2], smallest[3]));
+    return least;
 }
 
-// The list's n <= k items in descending order into one row of the outputs
-__device__ inline void put_sorted(const TopLds& l, int n, int k, float* values, int32_t* ids) {
+// Keeps the items of it[] that are not below `least` in the list, in any order; their number.  All threads, after a barrier behind the last
+// use of the list; two barriers.
+__device__ inline int keep_from(TopLds& l, const u64 (&it)[kTopItems], u64 least) {
+    if (threadIdx.x == 0) l.count = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kTopItems; ++i)
+        if (it[i] != 0 && it[i] >= least) l.list[atomicAdd(&l.count, 1)] = it[i];
+    __syncthreads();
+    return l.count;
+}
+
+// Brings the list's n <= 256 items into descending order and drops those behind the k-th; how many are left.  All threads.
+__device__ inline int sort_list(TopLds& l, int n, int k) {
     const int t = threadIdx.x;
-    if (t < n) {
-        const u64 mine = l.list[t];
-        int at = 0;
-        for (int i = 0; i < n; ++i) at += l.list[i] > mine;
-        values[at] = value_of((uint32_t)(mine >> 32));
-        ids[at] = (int32_t)~(uint32_t)mine;
+    const u64 mine = t < n ? l.list[t] : 0;
+    if (t == n && (n & 1)) l.list[n] = 0;   // pairs
+    __syncthreads();
+    int at = 0;
+#pragma unroll 4
+    for (int i = 0; i < n; i += 2) {
+        const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&l.list[i]);
+        at += (o.x > mine) + (o.y > mine);
     }
-    if (t >= n && t < k) {
-        values[t] = -INFINITY;
-        ids[t] = -1;
+    __syncthreads();
+    if (t < n && at < k) l.list[at] = mine;
+    if (t == 0) l.count = min(n, k);
+    __syncthreads();
+    return min(n, k);
+}
+
+// Cuts a list of n <= kTopList items to its k largest, in descending order; how many there are.  All threads, n uniform, after a barrier.
+__device__ inline int cut_list(TopLds& l, int n, int k) {
+    const int t = threadIdx.x;
+    if (n > kTopThreads) {
+        u64 it[kTopItems], mx = 0;
+#pragma unroll
+        for (int i = 0; i < kTopItems; ++i) {
+            it[i] = t + kTopThreads * i < n ? l.list[t + kTopThreads * i] : 0;
+            mx = max(mx, it[i]);
+        }
+        n = keep_from(l, it, (u64)kth_maximum(l, (uint32_t)(mx >> 32), k) << 32);
+        if (n > kTopThreads) {
+            __syncthreads();   // the count has been read
+            n = keep_from(l, it, kth_item(l, it, k));
+        }
     }
+    return sort_list(l, n, k);
+}
+
+// The list, sorted, into one row of the outputs
+__device__ inline void put_list(const TopLds& l, int n, int k, float* values, int32_t* ids) {
+    const int t = threadIdx.x;
+    if (t >= k) return;
+    const u64 it = t < n ? l.list[t] : 0;
+    values[t] = t < n ? value_of((uint32_t)(it >> 32)) : -INFINITY;
+    ids[t] = t < n ? (int32_t)~(uint32_t)it : -1;
 }
 
 __device__ inline float lse_of(float2 p, float inv_temp) { return p.y > 0.f ? (float)((double)p.x * inv_temp + (double)logf(p.y)) : -INFINITY; }
@@ -126,69 +191,71 @@ struct TopArgs {
 };
 
 template <bool BF16>
-__global__ __launch_bounds__(kTopThreads) void top_segment(const TopArgs a) {
+__global__ __launch_bounds__(kTopThreads, 4) void top_segment(const TopArgs a) {
     typedef Row<BF16> R;
     constexpr int N = R::N, VEC = kTopPer / N;
     __shared__ TopLds l;
     const int t = threadIdx.x, lane = t & 63, row = blockIdx.y, seg = blockIdx.x;
     const typename R::T* p = (const typename R::T*)a.in + (long long)row * a.stride;
     const int v0 = seg * a.seg_len, v1 = min(a.V, v0 + a.seg_len);
-    if (t == 0) l.count = 0, l.least = 0xffffffffu;
+    if (t == 0) l.count = 0;
+    const raw16 none = none16<BF16>();
+    auto load = [&](int b, raw16 (&r)[VEC]) {
+        if (b + kTopBlock <= v1) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) r[i] = (raw16)__builtin_nontemporal_load((const typename R::V*)(p + b + N * (t + kTopThreads * i)));
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const int v = b + N * (t + kTopThreads * i);
+                r[i] = v < v1 ? row_load<BF16>(p, v, v1) : none;
+            }
+        }
+    };
     float2 sum = make_float2(kNoEntry, 0.f);
     float from = kNoEntry;   // candidates are not below this: the lowest finite value shuts out -inf (and NaN)
     int n = 0, next_cut = 1;
-    for (int b = v0, done = 0; b < v1; b += kTopBlock) {
-        float z[kTopPer];
-        float mx = -INFINITY;
+    raw16 r[VEC], ahead[VEC];
+    load(v0, r);
+#pragma unroll 1
+    for (int b = v0, done = 1;; b += kTopBlock, ++done) {
+        const bool last = b + kTopBlock >= v1;
+        if (!last) load(b + kTopBlock, ahead);
+        float mx = kNoEntry;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const int v = b + N * (t + kTopThreads * i);
-            raw16 r;
-            if (v < v1) r = row_load<BF16>(p, v, v1);
-#pragma unroll
-            for (int x = 0; x < N; ++x) {
-                z[i * N + x] = v < v1 ? R::get(r, x) : -INFINITY;
-                mx = fmaxf(mx, z[i * N + x]);
-            }
-        }
+        for (int i = 0; i < VEC; ++i) mx = vec_max<BF16>(r[i], mx);
         if (a.lse) {
             const float m = fmaxf(sum.x, mx);
             float s = sum.y * fast_exp2((sum.x - m) * a.c2);
 #pragma unroll
-            for (int i = 0; i < kTopPer; ++i) s += fast_exp2((z[i] - m) * a.c2);
+            for (int i = 0; i < VEC; ++i) s = vec_sum<BF16>(r[i], m, a.c2, s);
             sum = make_float2(m, s);
         }
-        if (b == v0) {   // the k-th largest of the threads' maxima: k entries of this block at least reach it
-            l.maxima[t] = mx > -INFINITY ? rank_of(mx) : 0;
-            __syncthreads();
-            const uint32_t mine = l.maxima[t];
-            int above = 0;
-#pragma unroll 16
-            for (int i = 0; i < kTopThreads; ++i) above += l.maxima[i] > mine;
-            if (above < a.k && mine != 0) atomicMin(&l.least, mine);
-            __syncthreads();
-            int entries = 0;   // where fewer threads than k have an entry at all, the smallest of their maxima is no bound
-            for (int i = lane; i < kTopThreads; i += 64) entries += l.maxima[i] != 0;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) entries += __shfl_xor(entries, d);
-            if (entries >= a.k) from = value_of(l.least);
+        if (b == v0) {
+            // a thread without an entry above the lowest value counts as one without an entry: the bound only has to be reached by k others
+            const uint32_t bound = kth_maximum(l, mx > kNoEntry ? rank_of(mx) : 0, a.k);
+            if (bound > 1) from = value_of(bound);
         }
         if (mx >= from) {
 #pragma unroll
-            for (int i = 0; i < kTopPer; ++i)
-                if (z[i] >= from) l.list[atomicAdd(&l.count, 1)] = item_of(z[i], b + N * (t + kTopThreads * (i / N)) + i % N);
+            for (int i = 0; i < VEC; ++i)
+#pragma unroll
+                for (int x = 0; x < N; ++x) {
+                    const float z = R::get(r[i], x);
+                    if (z >= from) l.list[atomicAdd(&l.count, 1)] = item_of(z, b + N * (t + kTopThreads * i) + x);
+                }
         }
         __syncthreads();
         n = l.count;
-        ++done;
-        const bool last = b + kTopBlock >= v1;
-        if (n > a.k && (n > kTopLow || done == next_cut || last)) {
-            const u64 kth = cut_to(l, n, a.k);
-            n = a.k;
-            from = value_of((uint32_t)(kth >> 32) + 1u);
+        if (last || (n > a.k && (n > kTopLow || done == next_cut))) {
+            n = cut_list(l, n, a.k);
+            if (n == a.k) from = value_of((uint32_t)(l.list[a.k - 1] >> 32) + 1u);
         }
+        if (last) break;
         if (done == next_cut) next_cut *= 2;
         __syncthreads();   // the count has been read by all before the next block adds to it
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) r[i] = ahead[i];
     }
     if (a.lse) {
         const float m = wave_max_dpp(sum.x);
@@ -206,46 +273,52 @@ __global__ __launch_bounds__(kTopThreads) void top_segment(const TopArgs a) {
         u64* to = a.lists + ((long long)row * a.segs + seg) * a.k;
         if (t < a.k) to[t] = t < n ? l.list[t] : 0;
     } else {
-        put_sorted(l, n, a.k, a.values + (long long)row * a.k, a.ids + (long long)row * a.k);
+        put_list(l, n, a.k, a.values + (long long)row * a.k, a.ids + (long long)row * a.k);
     }
 }
 
 // one workgroup per row: the lists of its segments (their unused places are 0)
 __global__ __launch_bounds__(kTopThreads) void top_merge(const TopArgs a) {
     __shared__ TopLds l;
-    const int t = threadIdx.x, row = blockIdx.x;
-    const u64* from = a.lists + (long long)row * a.segs * a.k;
-    if (t == 0) l.count = 0;
-    __syncthreads();
-    for (int i = t; i < a.segs * a.k; i += kTopThreads) {
-        const u64 it = from[i];
-        if (it) l.list[atomicAdd(&l.count, 1)] = it;
+    const int t = threadIdx.x, lane = t & 63, row = blockIdx.x, all = a.segs * a.k;
+    const u64* from = a.lists + (long long)row * all;
+    u64 it[kTopItems], mx = 0;
+#pragma unroll
+    for (int i = 0; i < kTopItems; ++i) {
+        it[i] = t + kTopThreads * i < all ? from[t + kTopThreads * i] : 0;
+        mx = max(mx, it[i]);
     }
-    __syncthreads();
-    int n = l.count;
-    __syncthreads();
-    if (n > a.k) {
-        cut_to(l, n, a.k);
-        n = a.k;
+    float2 q = make_float2(kNoEntry, 0.f);
+    if (a.lse && t < 64)
+        for (int i = lane; i < a.segs; i += 64) q = join_sums(q, a.parts[(long long)row * a.segs + i], a.c2);
+    int n = keep_from(l, it, (u64)kth_maximum(l, (uint32_t)(mx >> 32), a.k) << 32);
+    if (n > kTopThreads) {
+        __syncthreads();
+        n = keep_from(l, it, kth_item(l, it, a.k));
     }
-    put_sorted(l, n, a.k, a.values + (long long)row * a.k, a.ids + (long long)row * a.k);
-    if (a.lse && t == 0) {
-        const float2* q = a.parts + (long long)row * a.segs;
-        float2 s = q[0];
-        for (int i = 1; i < a.segs; ++i) s = join_sums(s, q[i], a.c2);
-        a.lse[row] = lse_of(s, a.inv_temp);
+    n = sort_list(l, n, a.k);
+    put_list(l, n, a.k, a.values + (long long)row * a.k, a.ids + (long long)row * a.k);
+    if (a.lse && t < 64) {
+        const float m = wave_max_dpp(q.x);
+        const float s = wave_sum_dpp(q.y * fast_exp2((q.x - m) * a.c2));
+        if (t == 0) a.lse[row] = lse_of(make_float2(m, s), a.inv_temp);
     }
 }
 
-// Segments of a row: one where the rows alone give the chip two rounds of workgroups, else as many as that takes, each of a block at
-// least, and no more lists than one merging workgroup holds
+// Segments of a row: as many as make the call shortest, counted in blocks that pass one after the other.  1024 workgroups are on the chip at
+// once; a workgroup's start and its last cut take as long as one and a half blocks, the merging launch as long as three.
 static int top_segs(int n_rows, int vocab, int k) {
     const int blocks = (vocab + kTopBlock - 1) / kTopBlock;
-    int segs = (1024 + n_rows - 1) / n_rows;
-    if (segs > blocks) segs = blocks;
-    if (segs > kTopList / k) segs = kTopList / k;
-    const int len = (blocks + segs - 1) / segs;   // of equal length, in blocks
-    return (blocks + len - 1) / len;
+    int best = 1;
+    double least = 1e30;
+    for (int segs = 1; segs <= blocks && segs <= kTopList / k && segs <= 64; ++segs) {
+        const int len = (blocks + segs - 1) / segs;
+        if ((blocks + len - 1) / len != segs) continue;   // the same as fewer
+        const double rounds = (double)(((long long)n_rows * segs + 1023) / 1024);
+        const double cost = rounds * (len + 1.5) + (segs > 1 ? 3.0 : 0.0);
+        if (cost < least) least = cost, best = segs;
+    }
+    return best;
 }
 
 }  // namespace psd
