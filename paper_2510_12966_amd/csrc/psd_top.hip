@@ -1,12 +1,12 @@
 // The k largest entries of every row of logits, with the row's log-sum-exp.
 //
 // A workgroup streams over a segment of a row, 4096 entries at a time with the next ones on their way, and keeps a list of candidates in LDS:
-// entries not below a threshold that at least k entries of the segment are known to reach.  The first threshold is the k-th largest of the
-// threads' own maxima in the first block; whenever the list is cut to its k largest (after 1, 2, 4 ... blocks), their smallest becomes the
+// entries not below a threshold that at least k entries of the segment are known to reach.  The first threshold is one that k of the threads'
+// own maxima in the first block reach; whenever the list is cut to its k largest (after 2, 4, 8 ... blocks), their smallest becomes the
 // threshold, and later entries have to exceed it (an equal one has a higher token and comes behind).  So all but a few hundred entries of a
 // row cost a maximum, an exponential and their load.  Items are 64 bits (order-preserving image of the value, complement of the token)
-// and all differ, so that equal values fall in the order of their tokens by themselves.  A cut drops what is below the k-th largest of the
-// threads' maxima once more and ranks the rest by comparing all pairs, or, where more than 256 are left, by radix selection, 8 bits a round.
+// and all differ, so that equal values fall in the order of their tokens by themselves.  Ranks come from comparing all pairs of at most
+// 256 items; a longer list is first filtered by the threads' maxima again and, if that leaves too many, by radix selection, 8 bits a round.
 // Many rows: one segment each, one launch.  Few rows: several segments, whose lists a second launch merges.
 // Bound: the bytes of the rows, read once.
 #include "psd_rows.h"
@@ -57,23 +57,22 @@ __device__ inline uint32_t wave_max_u32(uint32_t v) {
     return max(p[0], p[1]);
 }
 
-// The k-th largest of the threads' maxima (images, 0: no entry), so at least k items reach it; 1 where fewer than k threads have one.
-// All threads; two barriers.
-__device__ inline uint32_t kth_maximum(TopLds& l, uint32_t mine, int k) {
-    const int t = threadIdx.x;
+// An image that at least k of the threads' maxima reach (0: no entry; 1 where that many have none): the least of the waves' ceil(k / 4)-th
+// largest.  Every thread counts the larger ones of its own wave.  All threads; one barrier.
+__device__ inline uint32_t reached_by(TopLds& l, uint32_t mine, int k) {
+    const int t = threadIdx.x, w = t >> 6;
     l.maxima[t] = mine;
-    const int have = __syncthreads_count(mine != 0);
-    if (have < k) return 1;   // uniform
     int above = 0;
-#pragma unroll 8
-    for (int i = 0; i < kTopThreads; i += 4) {
-        const uint4 o = *reinterpret_cast<const uint4*>(&l.maxima[i]);
+#pragma unroll
+    for (int i = 0; i < 64; i += 4) {
+        const uint4 o = *reinterpret_cast<const uint4*>(&l.maxima[64 * w + i]);
         above += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
     }
-    const uint32_t least = ~wave_max_u32(mine != 0 && above < k ? ~mine : 0u);
-    if ((t & 63) == 0) l.least[t >> 6] = least;
+    const int share = (k + 3) / 4;
+    const uint32_t least = ~wave_max_u32(above < share ? ~mine : 0u);   // (a lane without an entry is among them where the wave has too few)
+    if ((t & 63) == 0) l.least[w] = least;
     __syncthreads();
-    return min(min(l.least[0], l.least[1]), min(l.least[2], l.least[3]));
+    return max(min(min(l.least[0], l.least[1]), min(l.least[2], l.least[3])), 1u);
 }
 
 // Radix selection among the items it[] of all threads, of which more than k are not 0: the smallest of the k largest.  All threads.
@@ -129,6 +128,32 @@ __device__ inline int keep_from(TopLds& l, const u64 (&it)[kTopItems], u64 least
     return l.count;
 }
 
+// Drops from a list of n <= 256 items those that k others exceed in value, so that at least k are left; the k-th largest value's image where
+// there are k, else 1.  All threads, after a barrier; n becomes the number left, known after one more barrier.
+__device__ inline uint32_t tighten_list(TopLds& l, int n, int k) {
+    const int t = threadIdx.x, w = t >> 6;
+    const u64 it = t < n ? l.list[t] : 0;
+    const uint32_t mine = (uint32_t)(it >> 32);
+    l.maxima[t] = mine;
+    __syncthreads();
+    uint32_t least = ~0u;
+    if (64 * w < n) {   // waves that have items
+        int above = 0;
+#pragma unroll 4
+        for (int i = 0; i < n; i += 4) {
+            const uint4 o = *reinterpret_cast<const uint4*>(&l.maxima[i]);
+            above += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+        }
+        least = ~wave_max_u32(mine != 0 && above < k ? ~mine : 0u);
+    }
+    if ((t & 63) == 0) l.least[w] = least;
+    if (t == 0) l.count = 0;
+    __syncthreads();
+    least = n < k ? 1u : min(min(l.least[0], l.least[1]), min(l.least[2], l.least[3]));
+    if (mine >= least) l.list[atomicAdd(&l.count, 1)] = it;
+    return least;
+}
+
 // Brings the list's n <= 256 items into descending order and drops those behind the k-th; how many are left.  All threads.
 __device__ inline int sort_list(TopLds& l, int n, int k) {
     const int t = threadIdx.x;
@@ -136,10 +161,12 @@ __device__ inline int sort_list(TopLds& l, int n, int k) {
     if (t == n && (n & 1)) l.list[n] = 0;   // pairs
     __syncthreads();
     int at = 0;
+    if ((t & ~63) < n) {   // waves that have items
 #pragma unroll 4
-    for (int i = 0; i < n; i += 2) {
-        const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&l.list[i]);
-        at += (o.x > mine) + (o.y > mine);
+        for (int i = 0; i < n; i += 2) {
+            const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&l.list[i]);
+            at += (o.x > mine) + (o.y > mine);
+        }
     }
     __syncthreads();
     if (t < n && at < k) l.list[at] = mine;
@@ -158,7 +185,7 @@ __device__ inline int cut_list(TopLds& l, int n, int k) {
             it[i] = t + kTopThreads * i < n ? l.list[t + kTopThreads * i] : 0;
             mx = max(mx, it[i]);
         }
-        n = keep_from(l, it, (u64)kth_maximum(l, (uint32_t)(mx >> 32), k) << 32);
+        n = keep_from(l, it, (u64)reached_by(l, (uint32_t)(mx >> 32), k) << 32);
         if (n > kTopThreads) {
             __syncthreads();   // the count has been read
             n = keep_from(l, it, kth_item(l, it, k));
@@ -214,13 +241,13 @@ __global__ __launch_bounds__(kTopThreads, 4) void top_segment(const TopArgs a) {
     };
     float2 sum = make_float2(kNoEntry, 0.f);
     float from = kNoEntry;   // candidates are not below this: the lowest finite value shuts out -inf (and NaN)
-    int n = 0, next_cut = 1;
-    raw16 r[VEC], ahead[VEC];
-    load(v0, r);
-#pragma unroll 1
-    for (int b = v0, done = 1;; b += kTopBlock, ++done) {
+    int n = 0, next_cut = 2;
+    int done = 0;
+    // One block, then the load of the one after the next into the same registers: moving a block over would wait for it.  True: the last one.
+    auto step = [&](raw16 (&r)[VEC]) {
+        const int b = v0 + done * kTopBlock;
         const bool last = b + kTopBlock >= v1;
-        if (!last) load(b + kTopBlock, ahead);
+        ++done;
         float mx = kNoEntry;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) mx = vec_max<BF16>(r[i], mx);
@@ -231,32 +258,44 @@ __global__ __launch_bounds__(kTopThreads, 4) void top_segment(const TopArgs a) {
             for (int i = 0; i < VEC; ++i) s = vec_sum<BF16>(r[i], m, a.c2, s);
             sum = make_float2(m, s);
         }
-        if (b == v0) {
+        if (done == 1) {
             // a thread without an entry above the lowest value counts as one without an entry: the bound only has to be reached by k others
-            const uint32_t bound = kth_maximum(l, mx > kNoEntry ? rank_of(mx) : 0, a.k);
+            const uint32_t bound = reached_by(l, mx > kNoEntry ? rank_of(mx) : 0, a.k);
             if (bound > 1) from = value_of(bound);
         }
-        if (mx >= from) {
+        if (mx >= from) {   // one place in the list per thread and block, whatever it brings
+            int brings = 0;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+#pragma unroll
+                for (int x = 0; x < N; ++x) brings += R::get(r[i], x) >= from;
+            int at = atomicAdd(&l.count, brings);
 #pragma unroll
             for (int i = 0; i < VEC; ++i)
 #pragma unroll
                 for (int x = 0; x < N; ++x) {
                     const float z = R::get(r[i], x);
-                    if (z >= from) l.list[atomicAdd(&l.count, 1)] = item_of(z, b + N * (t + kTopThreads * i) + x);
+                    if (z >= from) l.list[at++] = item_of(z, b + N * (t + kTopThreads * i) + x);
                 }
         }
+        if (b + 2 * kTopBlock < v1) load(b + 2 * kTopBlock, r);
         __syncthreads();
         n = l.count;
-        if (last || (n > a.k && (n > kTopLow || done == next_cut))) {
+        if (last || n > kTopLow) {
             n = cut_list(l, n, a.k);
             if (n == a.k) from = value_of((uint32_t)(l.list[a.k - 1] >> 32) + 1u);
+        } else if (n > a.k && done >= next_cut) {
+            const uint32_t kth = tighten_list(l, n, a.k);
+            if (kth > 1) from = value_of(kth + 1u);
         }
-        if (last) break;
-        if (done == next_cut) next_cut *= 2;
+        if (done >= next_cut) next_cut = 2 * done;
         __syncthreads();   // the count has been read by all before the next block adds to it
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) r[i] = ahead[i];
-    }
+        return last;
+    };
+    raw16 even[VEC], odd[VEC];
+    load(v0, even);
+    if (v0 + kTopBlock < v1) load(v0 + kTopBlock, odd);
+    while (!step(even) && !step(odd)) {}
     if (a.lse) {
         const float m = wave_max_dpp(sum.x);
         const float s = wave_sum_dpp(sum.y * fast_exp2((sum.x - m) * a.c2));
@@ -291,7 +330,7 @@ __global__ __launch_bounds__(kTopThreads) void top_merge(const TopArgs a) {
     float2 q = make_float2(kNoEntry, 0.f);
     if (a.lse && t < 64)
         for (int i = lane; i < a.segs; i += 64) q = join_sums(q, a.parts[(long long)row * a.segs + i], a.c2);
-    int n = keep_from(l, it, (u64)kth_maximum(l, (uint32_t)(mx >> 32), a.k) << 32);
+    int n = keep_from(l, it, (u64)reached_by(l, (uint32_t)(mx >> 32), a.k) << 32);
     if (n > kTopThreads) {
         __syncthreads();
         n = keep_from(l, it, kth_item(l, it, a.k));
