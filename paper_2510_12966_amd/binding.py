@@ -173,9 +173,10 @@ def _dev_ptr(a):
     """Address of a device buffer; host arrays are refused (a kernel must not be given their addresses)."""
     if a is None:
         return None
-    if not hasattr(a, "data_ptr"):
-        raise TypeError(f"a device buffer (an object with data_ptr()) is needed, not {type(a).__name__}")
-    return a.data_ptr() or None
+    try:
+        return a.data_ptr() or None
+    except AttributeError:
+        raise TypeError(f"a device buffer (an object with data_ptr()) is needed, not {type(a).__name__}") from None
 
 
 class DeviceBuffer:

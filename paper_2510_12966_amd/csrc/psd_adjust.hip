@@ -2,21 +2,22 @@
 //
 // One launch.  A workgroup takes one chunk of the vocabulary of one sequence and some of the sequence's rows.  It counts the
 // occurrences of the chunk's tokens in the history (integer atomics in LDS: the counts do not depend on their order), finds the last bias
-// given for each (an atomic maximum of places in the list), and then goes through its rows, adding one token of the window
-// after each.  Bound: the bytes of the rows, read once and written once.
+// given for each (an atomic maximum of places in the list), and then goes through its rows, the next one on its way while one is written,
+// adding one token of the window after each.  Bound: the bytes of the rows, read once and written once, where histories are short; every
+// chunk's workgroups go through the whole history, which is why long ones get larger chunks.
 #include "psd_rows.h"
 
 namespace psd {
 
-constexpr int kAdjThreads = 256;
-constexpr int kAdjChunk = 4096;         // vocabulary entries of a workgroup: 16 KB of counts and as much of biases
+constexpr int kAdjPer = 16;             // entries of a row that a thread has
 constexpr uint32_t kPromptOnly = 0x80000000u;   // a count word: occurrences that count for presence and frequency, and this bit where
                                                 // the token stands in the uncounted part of the history: 0 means it never occurred
 
 struct AdjustArgs {
     const void* in;
     void* out;
-    int rows, V, group;   // group: rows of a sequence that one workgroup goes through
+    int rows, V, group;    // group: rows of a sequence that one workgroup goes through
+    int counts, biases;    // 0 or 1: whether there are counts and biases to keep
     long long in_stride, out_stride;
     psd_adjust a;
 };
@@ -29,104 +30,205 @@ __device__ inline void list_of(const int64_t* offsets, int s, int64_t n, int64_t
     hi = hi < lo ? lo : hi > n ? n : hi;
 }
 
-template <bool BF16>
-__global__ __launch_bounds__(kAdjThreads) void adjust_rows(const AdjustArgs g) {
-    typedef Row<BF16> R;
-    constexpr int N = R::N, VEC = kAdjChunk / (N * kAdjThreads);   // vectors of a row that a thread has: 4 or 2
-    __shared__ uint32_t count[kAdjChunk];
-    __shared__ uint32_t bias[kAdjChunk];   // places in the list (from 1 on), then the biases themselves
+typedef int32_t four_tokens __attribute__((ext_vector_type(4), aligned(4)));
+
+struct Penalty { float repetition, inverse, presence, frequency; };   // inverse: 1 / repetition
+
+// One logit.  The quotient comes from the rounded inverse and one correction by its remainder (exact in the fused multiply-add).
+__device__ inline float adjusted(float z, uint32_t count, const Penalty& p) {
+    const float q = z * p.inverse, quotient = __builtin_amdgcn_div_fixupf(fmaf(fmaf(-q, p.repetition, z), p.inverse, q), p.repetition, z);
+    const float y = z > 0.f ? quotient : z * p.repetition;
+    const uint32_t occurrences = count & ~kPromptOnly;
+    const float minus = occurrences ? fmaf((float)occurrences, p.frequency, p.presence) : 0.f;
+    return count ? y - minus : z;
+}
+
+// What the lists say about the n entries from v0 on: occurrences in the history and in the window's first j0 tokens, and biases.  All threads,
+// after the counts and biases have been cleared; a barrier at its end.
+template <int NT>
+__device__ inline void read_lists(const AdjustArgs& g, uint32_t* count, uint32_t* bias, const int32_t* window, int s, int v0, int n, int j0) {
+    constexpr int AHEAD = 4;
     const psd_adjust& a = g.a;
-    const int s = blockIdx.z, v0 = blockIdx.x * kAdjChunk, n = min(kAdjChunk, g.V - v0);
-    const int j0 = blockIdx.y * g.group, j1 = min(g.rows, j0 + g.group);
     const int t = threadIdx.x;
-    int64_t h0 = 0, h1 = 0, b0 = 0, b1 = 0;
-    if (a.history) list_of(a.history_offsets, s, a.n_history, h0, h1);
-    if (a.bias) list_of(a.bias_offsets, s, a.n_bias, b0, b1);
-    for (int i = t; i < kAdjChunk; i += kAdjThreads) count[i] = 0, bias[i] = 0;
-    __syncthreads();
-    const int64_t counted = h0 + (a.n_prompt ? max(0, a.n_prompt[s]) : 0);
-    for (int64_t i = h0 + t; i < h1; i += kAdjThreads) {
-        const uint32_t u = (uint32_t)a.history[i] - (uint32_t)v0;
-        if (u >= (uint32_t)n) continue;
-        if (i >= counted) atomicAdd(&count[u], 1u);
-        else atomicOr(&count[u], kPromptOnly);
+    // the first of the biases (all of them, most of the time) set out first
+    int64_t b0 = 0, b1 = 0;
+    int32_t btok = -1;
+    float bval = 0.f;
+    if (a.bias) {
+        list_of(a.bias_offsets, s, a.n_bias, b0, b1);
+        if (b0 + t < b1) btok = a.bias_tokens[b0 + t], bval = a.bias[b0 + t];
     }
-    const int32_t* window = a.window ? a.window + (int64_t)s * a.window_stride : nullptr;
+    if (a.history) {
+        int64_t lo, hi;
+        list_of(a.history_offsets, s, a.n_history, lo, hi);
+        const int64_t counted = lo + (a.n_prompt ? max(0, a.n_prompt[s]) : 0);
+        for (int64_t i0 = lo; i0 < hi; i0 += 4 * NT * AHEAD) {
+            int32_t tok[AHEAD][4];
+#pragma unroll
+            for (int x = 0; x < AHEAD; ++x) {
+                const int64_t i = i0 + 4 * (t + NT * x);
+                if (i + 4 <= hi) {
+                    const four_tokens f = *reinterpret_cast<const four_tokens*>(a.history + i);
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) tok[x][y] = f[y];
+                } else {
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) tok[x][y] = i + y < hi ? a.history[i + y] : -1;
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < AHEAD; ++x)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const uint32_t u = (uint32_t)tok[x][y] - (uint32_t)v0;
+                    if (u >= (uint32_t)n) continue;
+                    if (i0 + 4 * (t + NT * x) + y >= counted) atomicAdd(&count[u], 1u);
+                    else atomicOr(&count[u], kPromptOnly);
+                }
+        }
+    }
     if (window)
-        for (int i = t; i < j0; i += kAdjThreads) {
+        for (int i = t; i < j0; i += NT) {
             const uint32_t u = (uint32_t)window[i] - (uint32_t)v0;
             if (u < (uint32_t)n) atomicAdd(&count[u], 1u);
         }
-    for (int64_t i = b0 + t; i < b1; i += kAdjThreads) {
-        const uint32_t u = (uint32_t)a.bias_tokens[i] - (uint32_t)v0;
-        if (u < (uint32_t)n) atomicMax(&bias[u], (uint32_t)(i - b0) + 1u);
-    }
-    __syncthreads();
-    if (b1 > b0) {
-        for (int i = t; i < n; i += kAdjThreads) {
-            const uint32_t at = bias[i];
-            bias[i] = at ? __float_as_uint(a.bias[b0 + at - 1]) : 0u;
+    if (a.bias) {
+        const uint32_t u = (uint32_t)btok - (uint32_t)v0;
+        if (u < (uint32_t)n) atomicMax(&bias[u], (uint32_t)t + 1u);
+        for (int64_t i = b0 + NT + t; i < b1; i += NT) {
+            const uint32_t w = (uint32_t)a.bias_tokens[i] - (uint32_t)v0;
+            if (w < (uint32_t)n) atomicMax(&bias[w], (uint32_t)(i - b0) + 1u);
         }
         __syncthreads();
-    }
-    float rep = 1.f, presence = 0.f, frequency = 0.f;
-    if (a.penalties) {
-        rep = a.penalties[3 * s];
-        presence = a.penalties[3 * s + 1];
-        frequency = a.penalties[3 * s + 2];
-        if (!(rep > 0.f)) rep = 1.f;
-    }
-    const int words = (g.V + 31) >> 5;
-    for (int j = j0; j < j1; ++j) {
-        const long long r = (long long)s * g.rows + j;
-        const typename R::T* row = (const typename R::T*)g.in + r * g.in_stride;
-        typename R::T* to = (typename R::T*)g.out + r * g.out_stride;
-        const uint32_t* mask = nullptr;
-        bool closed = false;
-        if (a.mask_index) {
-            const int m = a.mask_index[r];
-            if (m >= 0 && m < a.n_masks) mask = a.masks + (long long)m * words;
-            else closed = m != -1;
-        }
-        raw16 z[VEC];
-        uint32_t open[VEC];
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const int v = v0 + N * (t + kAdjThreads * i);
-            open[i] = closed ? 0u : 0xffffffffu;
-            if (v < g.V) {
-                z[i] = row_load<BF16>(row, v, g.V);
-                if (mask) open[i] = mask[v >> 5] >> (v & 31);
+        if (b1 - b0 <= NT) {   // the places' own threads put the values there, once all have looked
+            const bool counts = u < (uint32_t)n && bias[u] == (uint32_t)t + 1u;
+            __syncthreads();
+            if (counts) bias[u] = __float_as_uint(bval);
+        } else {
+            for (int i = t; i < n; i += NT) {
+                const uint32_t at = bias[i];
+                if (at) bias[i] = __float_as_uint(a.bias[b0 + at - 1]);
             }
         }
+    }
+    __syncthreads();
+}
+
+// The rows j0 .. j1 - 1 of a chunk: WHOLE where it lies inside the vocabulary.  Two rows are on their way while one is written; their registers
+// take turns (moving a row over would wait for it).
+template <bool BF16, int NT, bool WHOLE>
+__device__ inline void adjust_group(const AdjustArgs& g, uint32_t* count, uint32_t* bias, const Penalty& pen, int s, int v0, int j0, int j1) {
+    typedef Row<BF16> R;
+    typedef typename R::T T;
+    constexpr int N = R::N, VEC = kAdjPer / N;
+    const psd_adjust& a = g.a;
+    const int t = threadIdx.x, words = (g.V + 31) >> 5, n = WHOLE ? kAdjPer * NT : g.V - v0;
+    const long long row0 = (long long)s * g.rows;
+    auto mask_of = [&](int j) { return a.mask_index && j < j1 ? a.mask_index[row0 + j] : -1; };   // asked for a row ahead of its use
+    auto load = [&](int j, int m, raw16 (&z)[VEC], uint32_t (&open)[VEC]) {
+        const T* row = (const T*)g.in + (row0 + j) * g.in_stride + v0;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            const int u = N * (t + kAdjThreads * i), v = v0 + u;
-            if (v >= g.V) continue;
+            const int u = N * (t + NT * i);
+            if (WHOLE) z[i] = (raw16)__builtin_nontemporal_load((const typename R::V*)(row + u));
+            else if (u < n) z[i] = row_load<BF16>(row, u, n);
+        }
+        const bool masked = m >= 0 && m < a.n_masks;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) open[i] = m == -1 ? 0xffffffffu : 0u;
+        if (masked) {
+            const uint32_t* mask = a.masks + (long long)m * words + (v0 >> 5);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const int u = N * (t + NT * i);
+                if (WHOLE || u < n) open[i] = mask[u >> 5] >> (u & 31);
+            }
+        }
+    };
+    raw16 even[VEC], odd[VEC];
+    uint32_t open_even[VEC], open_odd[VEC];
+    int j = j0, m_next = mask_of(j0 + 2);
+    load(j0, mask_of(j0), even, open_even);
+    if (j0 + 1 < j1) load(j0 + 1, mask_of(j0 + 1), odd, open_odd);
+    const int32_t* window = a.window ? a.window + (int64_t)s * a.window_stride : nullptr;
+    __syncthreads();
+    read_lists<NT>(g, count, bias, window, s, v0, n, j0);
+    auto step = [&](raw16 (&z)[VEC], uint32_t (&open)[VEC]) {   // true: the last row
+        T* to = (T*)g.out + (row0 + j) * g.out_stride + v0;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const int u = N * (t + NT * i);
             float e[N];
 #pragma unroll
-            for (int x = 0; x < N; ++x) {
-                float y = R::get(z[i], x);
-                const uint32_t c = count[u + x];
-                if (c) {
-                    y = y > 0.f ? y / rep : y * rep;
-                    const uint32_t occurrences = c & ~kPromptOnly;
-                    if (occurrences) y = y - fmaf((float)occurrences, frequency, presence);
+            for (int x = 0; x < N; ++x) e[x] = R::get(z[i], x);
+            if (g.counts) {
+#pragma unroll
+                for (int q = 0; q < N; q += 4) {
+                    const uint4 c = *reinterpret_cast<const uint4*>(&count[u + q]);
+                    e[q] = adjusted(e[q], c.x, pen);
+                    e[q + 1] = adjusted(e[q + 1], c.y, pen);
+                    e[q + 2] = adjusted(e[q + 2], c.z, pen);
+                    e[q + 3] = adjusted(e[q + 3], c.w, pen);
                 }
-                y = y + __uint_as_float(bias[u + x]);
-                e[x] = (open[i] >> x) & 1 ? y : -INFINITY;
             }
-            row_store<BF16>(to, v, g.V, e);
-        }
-        if (window && j + 1 < j1) {
-            __syncthreads();
-            if (t == 0) {
-                const uint32_t u = (uint32_t)window[j] - (uint32_t)v0;
-                if (u < (uint32_t)n) count[u] += 1;
+            if (g.biases) {
+#pragma unroll
+                for (int q = 0; q < N; q += 4) {
+                    const float4 b = *reinterpret_cast<const float4*>(&bias[u + q]);
+                    e[q] += b.x;
+                    e[q + 1] += b.y;
+                    e[q + 2] += b.z;
+                    e[q + 3] += b.w;
+                }
             }
-            __syncthreads();
+#pragma unroll
+            for (int x = 0; x < N; ++x) e[x] = (open[i] >> x) & 1 ? e[x] : -INFINITY;
+            if (WHOLE) __builtin_nontemporal_store((typename R::V)R::pack(e), (typename R::V*)(to + u));
+            else if (u < n) row_store<BF16>(to, u, n, e);
         }
+        if (j + 2 < j1) {
+            load(j + 2, m_next, z, open);
+            m_next = mask_of(j + 3);
+        }
+        if (j + 1 >= j1) return true;
+        if (window) {
+            const uint32_t u = (uint32_t)window[j] - (uint32_t)v0;
+            if (u < (uint32_t)n) {   // the same for all threads
+                __syncthreads();
+                if (t == 0) count[u] += 1;
+                __syncthreads();
+            }
+        }
+        ++j;
+        return false;
+    };
+    while (!step(even, open_even) && !step(odd, open_odd)) {}
+}
+
+template <bool BF16, int NT>
+__global__ __launch_bounds__(NT, 4) void adjust_rows(const AdjustArgs g) {
+    constexpr int CHUNK = kAdjPer * NT;
+    extern __shared__ uint4 lds[];
+    uint32_t* const count = reinterpret_cast<uint32_t*>(lds);
+    uint32_t* const bias = count + (g.counts ? CHUNK : 0);   // places in the list (from 1 on), then the biases themselves
+    // the sequence is the fastest index: workgroups go round the dies, and the chunks of one sequence read its history out of the same L2
+    const int s = blockIdx.x, v0 = blockIdx.z * CHUNK, j0 = blockIdx.y * g.group, j1 = min(g.rows, j0 + g.group);
+    for (int i = threadIdx.x; i < (g.counts + g.biases) * (CHUNK / 4); i += NT) lds[i] = make_uint4(0, 0, 0, 0);
+    Penalty pen{1.f, 1.f, 0.f, 0.f};
+    if (g.a.penalties) {
+        const float* p = g.a.penalties + 3 * (int64_t)s;
+        const float r = p[0] > 0.f ? p[0] : 1.f;
+        pen = Penalty{r, 1.f / r, p[1], p[2]};
     }
+    if (v0 + CHUNK <= g.V) adjust_group<BF16, NT, true>(g, count, bias, pen, s, v0, j0, j1);
+    else adjust_group<BF16, NT, false>(g, count, bias, pen, s, v0, j0, j1);
+}
+
+template <bool BF16, int NT>
+static void adjust_launch(AdjustArgs& g, int n_seqs, hipStream_t st) {
+    const int chunks = (g.V + kAdjPer * NT - 1) / (kAdjPer * NT);
+    const dim3 grid(n_seqs, (g.rows + g.group - 1) / g.group, chunks);
+    adjust_rows<BF16, NT><<<grid, NT, (size_t)(g.counts + g.biases) * kAdjPer * NT * 4, st>>>(g);
 }
 
 }  // namespace psd
@@ -145,7 +247,7 @@ extern "C" int psd_adjust_logits(const void* logits, void* out, int32_t dtype, i
     if (rc != PSD_OK) return rc;
     if (!rows_apart_or_same(logits, logits_stride, out, out_stride, n, vocab, row_elem(dtype)))
         PSD_FAIL(PSD_EINVAL, err, "%s: out overlaps the logits", who);
-    AdjustArgs g{logits, out, rows, vocab, rows, logits_stride, out_stride, *adjust};
+    AdjustArgs g{logits, out, rows, vocab, rows, 0, 0, logits_stride, out_stride, *adjust};
     psd_adjust& a = g.a;
     if (a.n_history < 0 || a.n_bias < 0 || a.n_masks < 0 || a.n_masks > 0x7fffffffLL || a.n_bias > 0x7fffffffLL)
         PSD_FAIL(PSD_EINVAL, err, "%s: n_history=%lld n_bias=%lld n_masks=%lld", who, (long long)a.n_history, (long long)a.n_bias, (long long)a.n_masks);
@@ -160,12 +262,22 @@ extern "C" int psd_adjust_logits(const void* logits, void* out, int32_t dtype, i
     if (a.n_history == 0) a.history = nullptr;
     if (a.n_bias == 0) a.bias = nullptr;
     if (rows == 1) a.window = nullptr;
-    const int chunks = (vocab + kAdjChunk - 1) / kAdjChunk;
-    // Every workgroup goes through the history again, so a sequence's rows stay together, unless that leaves the chip short of workgroups
-    while (g.group > 1 && (long long)chunks * n_seqs * ((rows + g.group - 1) / g.group) < 1024) g.group = (g.group + 1) / 2;
-    const dim3 grid(chunks, (rows + g.group - 1) / g.group, n_seqs);
-    if (dtype == PSD_BF16) adjust_rows<true><<<grid, kAdjThreads, 0, (hipStream_t)stream>>>(g);
-    else adjust_rows<false><<<grid, kAdjThreads, 0, (hipStream_t)stream>>>(g);
+    // without penalties occurrences change nothing
+    if (!a.penalties) a.history = nullptr, a.window = nullptr;
+    g.counts = a.history || a.window;
+    g.biases = a.bias != nullptr;
+    // Chunks of 4096 entries; of 16384 (a workgroup of 1024 threads per unit) where histories are long, for every chunk reads all of its
+    // sequence's (us, 4096 / 16384; one bf16 row of 128256 for each of 64 sequences: 30000 tokens 33.9 / 20.8, 3000 tokens 15.1 / 15.7)
+    const bool large = a.history && a.n_history / n_seqs > 4096;
+    // Every group of rows reads the lists again and leaves a workgroup more: groups of one row as long as the chip is not full, larger ones then (us;
+    // 32 rows of 32000 for 8 sequences: 1 / 2 / 5 rows a group 16.1 / 14.6 / 18.9; 9 rows of 128256 for 48: 98 / 93 / 91)
+    const long long chunks = (vocab + (large ? 16383 : 4095)) / (large ? 16384 : 4096), most = (n * vocab * row_elem(dtype) < 64LL << 20 ? 1024 : 3072) / (large ? 4 : 1);
+    long long groups = most / (chunks * n_seqs);
+    groups = groups < 1 ? 1 : groups > rows ? rows : groups;
+    g.group = (int)((rows + groups - 1) / groups);
+    hipStream_t st = (hipStream_t)stream;
+    if (dtype == PSD_BF16) large ? adjust_launch<true, 1024>(g, n_seqs, st) : adjust_launch<true, 256>(g, n_seqs, st);
+    else large ? adjust_launch<false, 1024>(g, n_seqs, st) : adjust_launch<false, 256>(g, n_seqs, st);
     PSD_HIP(hipGetLastError(), err);
     return PSD_OK;
 }
