@@ -44,8 +44,8 @@ struct DistillArgs {
 
 // What the workgroup keeps of a record: a thread of the first four waves ("place threads") has a place
 struct PlaceLds {
-    int ids[kPlaces];
-    int list[kPlaces], n_list, n_found;  // places that share 16 bytes of the row (or look as if)
+    int2 list[kPlaces];                  // (token, place) of places that share 16 bytes of the row (or look as if)
+    int n_list, n_found;
     float es[kPlaces];                   // student: 2^((z - z_max) c2), 0 where the place does not count
     float p[kPlaces];                    // teacher: probability times p_sum
     float z_max[kPlaceWaves], t_max[kPlaceWaves];
@@ -107,10 +107,8 @@ __device__ inline double log_share(float x, float y) {
 // Tokens of the same 16 bytes differ in the bits below N only; places that merely share a bit of the table drop out by their tokens.
 template <typename W>
 __device__ inline bool place_enter(PlaceLds& l, int id, W* word, W bit) {
-    const int t = threadIdx.x;
-    l.ids[t] = id;
     if (!bit || !(atomicOr(word, bit) & bit)) return false;
-    l.list[atomicAdd(&l.n_list, 1)] = t;
+    l.list[atomicAdd(&l.n_list, 1)] = make_int2(id, (int)threadIdx.x);
     return true;
 }
 // all threads, after a barrier; entered: in a place thread with a token, listed: place_enter's answer.  The flags of this place.
@@ -119,19 +117,32 @@ __device__ inline uint32_t place_flags(PlaceLds& l, int id, bool entered, bool l
     const int t = threadIdx.x, n = l.n_list;
     uint32_t flags = entered ? kHere | kOwner | 1u << (id & (N - 1)) : 0u;
     if (n == 0) return flags;
+    const int none = id ^ (1 << 30);   // (differs from id by far more than N)
     bool meets = false;
     if (entered && !listed)
-        for (int i = 0; i < n; ++i) meets |= ((uint32_t)l.ids[l.list[i]] ^ (uint32_t)id) < (uint32_t)N;
-    if (meets) l.list[n + atomicAdd(&l.n_found, 1)] = t;
-    __syncthreads();
-    if (listed || meets)
-        for (int i = 0; i < n + l.n_found; ++i) {
-            const int o = l.list[i];
-            const uint32_t x = (uint32_t)l.ids[o] ^ (uint32_t)id;
-            if (x >= (uint32_t)N) continue;
-            flags |= 1u << (((uint32_t)id ^ x) & (N - 1));
-            if (o < t) flags &= x == 0 ? ~(kHere | kOwner) : ~kOwner;
+        for (int i = 0; i < n; i += 8) {   // eight at a time: their reads need not wait for each other
+            int o[8];
+#pragma unroll
+            for (int y = 0; y < 8; ++y) o[y] = i + y < n ? l.list[i + y].x : none;
+#pragma unroll
+            for (int y = 0; y < 8; ++y) meets |= ((uint32_t)o[y] ^ (uint32_t)id) < (uint32_t)N;
         }
+    if (meets) l.list[n + atomicAdd(&l.n_found, 1)] = make_int2(id, t);
+    __syncthreads();
+    if (listed || meets) {
+        const int all = n + l.n_found;
+        for (int i = 0; i < all; i += 8) {
+            int2 o[8];
+#pragma unroll
+            for (int y = 0; y < 8; ++y) o[y] = i + y < all ? l.list[i + y] : make_int2(none, t);
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+                const uint32_t x = (uint32_t)o[y].x ^ (uint32_t)id;
+                flags |= x < (uint32_t)N ? 1u << (((uint32_t)id ^ x) & (N - 1)) : 0u;
+                flags &= x < (uint32_t)N && o[y].y < t ? (x == 0 ? ~(kHere | kOwner) : ~kOwner) : ~0u;
+            }
+        }
+    }
     return flags & kHere ? flags : 0u;
 }
 

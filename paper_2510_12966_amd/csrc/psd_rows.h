@@ -6,7 +6,7 @@
 namespace psd {
 
 constexpr int kMaxRows = 65535;       // rows of a call, as in psd_sample and psd_row_stats
-constexpr int kMaxVocab = 1 << 28;    // keeps every index of a row, rounded up to whole chunks, inside 32 bits
+constexpr int kMaxVocab = 1 << 27;    // keeps every index of a row, rounded up to whole chunks, inside 32 bits
 
 // Sums of exponentials are kept with the largest logit of their range, sum 2^((z - max) c2): the difference first, so that rows whose
 // every entry is the type's lowest value still have a distribution.  A range without an entry above -inf has the lowest finite maximum

@@ -2,11 +2,12 @@
 //
 // A workgroup streams over a segment of a row, 4096 entries at a time with the next ones on their way, and keeps a list of candidates in LDS:
 // entries not below a threshold that at least k entries of the segment are known to reach.  The first threshold is one that k of the threads'
-// own maxima in the first block reach; whenever the list is cut to its k largest (after 2, 4, 8 ... blocks), their smallest becomes the
-// threshold, and later entries have to exceed it (an equal one has a higher token and comes behind).  So all but a few hundred entries of a
-// row cost a maximum, an exponential and their load.  Items are 64 bits (order-preserving image of the value, complement of the token)
-// and all differ, so that equal values fall in the order of their tokens by themselves.  Ranks come from comparing all pairs of at most
-// 256 items; a longer list is first filtered by the threads' maxima again and, if that leaves too many, by radix selection, 8 bits a round.
+// own maxima in the first block reach.  Entries that enter the list are counted in 256 bins by value, and the lower edge of the bin in which the
+// k-th largest lies is the next threshold; a list that grows too long is freed of what lies below it.  So all but a few hundred entries of a
+// row cost a maximum, an exponential and their load.  What is left at the end, or where the bins cannot tell values apart, is cut exactly: ranks
+// come from comparing all pairs of at most 256 items, before that a longer list is filtered by the threads' maxima and, if that leaves too many, by
+// radix selection, 8 bits a round.  Items are 64 bits (order-preserving image of the value, complement of the token) and all differ, so that
+// equal values fall in the order of their tokens by themselves.
 // Many rows: one segment each, one launch.  Few rows: several segments, whose lists a second launch merges.
 // Bound: the bytes of the rows, read once.
 #include "psd_rows.h"
@@ -16,9 +17,9 @@ namespace psd {
 constexpr int kTopThreads = 256;
 constexpr int kTopBlock = 4096;                       // entries between two looks at the list
 constexpr int kTopPer = kTopBlock / kTopThreads;      // of one thread: 16
-constexpr int kTopLow = 256;                          // a list longer than this is cut before the next block
+constexpr int kTopLow = 480;                          // a list longer than this is cut before the next block
 constexpr int kTopList = kTopLow + kTopBlock;         // so every entry of a block finds a place in it
-constexpr int kTopItems = kTopList / kTopThreads;     // 17
+constexpr int kTopItems = (kTopList + kTopThreads - 1) / kTopThreads;   // 18
 static_assert(PSD_MAX_TOP <= kTopThreads && PSD_MAX_TOP <= kTopLow, "a thread, and a place in a cut list, per entry of the result");
 
 typedef unsigned long long u64;
@@ -33,10 +34,13 @@ __device__ inline u64 item_of(float z, int v) { return (u64)rank_of(z) << 32 | (
 
 struct TopLds {
     alignas(16) u64 list[kTopList];
-    uint32_t hist[3][256];   // one is filled, the next cleared, the last may still be read
-    alignas(16) uint32_t maxima[kTopThreads];
+    alignas(16) uint32_t bins[256];
+    union {   // (barriers lie between the uses of one and of the other)
+        uint32_t hist[3][256];   // one is filled, the next cleared, the last may still be read
+        alignas(16) uint32_t maxima[kTopThreads];
+    };
     float2 part[kTopThreads / 64];
-    uint32_t least[kTopThreads / 64];
+    alignas(16) uint4 least[kTopThreads / 64];
     u64 smallest[kTopThreads / 64];
     int count;
 };
@@ -57,22 +61,44 @@ __device__ inline uint32_t wave_max_u32(uint32_t v) {
     return max(p[0], p[1]);
 }
 
-// An image that at least k of the threads' maxima reach (0: no entry; 1 where that many have none): the least of the waves' ceil(k / 4)-th
-// largest.  Every thread counts the larger ones of its own wave.  All threads; one barrier.
+// sum over the lanes up to and including each
+template <int CTRL, int ROW_MASK>
+__device__ inline int sum_moved(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROW_MASK, 0xf, false); }
+__device__ inline int wave_scan(int v) {
+    v = sum_moved<0x111, 0xf>(v);   // row_shr:1
+    v = sum_moved<0x112, 0xf>(v);   // row_shr:2
+    v = sum_moved<0x114, 0xf>(v);   // row_shr:4
+    v = sum_moved<0x118, 0xf>(v);   // row_shr:8
+    v = sum_moved<0x142, 0xa>(v);   // row_bcast15 into rows 1 and 3
+    return sum_moved<0x143, 0xc>(v);   // row_bcast31 into rows 2 and 3
+}
+
+// An image that at least k of the threads' maxima reach (0: no entry; 1 where that many have none): in every wave a quarter of k, or half of k in
+// two, or all k in one (short and masked rows leave waves without entries).  Every thread counts the larger ones of its own wave.  All threads;
+// one barrier.
 __device__ inline uint32_t reached_by(TopLds& l, uint32_t mine, int k) {
     const int t = threadIdx.x, w = t >> 6;
     l.maxima[t] = mine;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     int above = 0;
 #pragma unroll
     for (int i = 0; i < 64; i += 4) {
         const uint4 o = *reinterpret_cast<const uint4*>(&l.maxima[64 * w + i]);
         above += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
     }
-    const int share = (k + 3) / 4;
-    const uint32_t least = ~wave_max_u32(above < share ? ~mine : 0u);   // (a lane without an entry is among them where the wave has too few)
-    if ((t & 63) == 0) l.least[w] = least;
+    uint32_t least[3];   // the wave's ceil(k / 4)-th, ceil(k / 2)-th and k-th largest, 0 where it has too few
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        const int share = (k + (4 >> i) - 1) / (4 >> i);
+        least[i] = share > 64 ? 0u : ~wave_max_u32(above < share ? ~mine : 0u);   // (a lane without an entry is among them where the wave has too few)
+    }
+    const uint32_t most = wave_max_u32(mine);
+    if ((t & 63) == 0) l.least[w] = make_uint4(least[0], least[1], least[2], most);
     __syncthreads();
-    return max(min(min(l.least[0], l.least[1]), min(l.least[2], l.least[3])), 1u);
+    const uint4 q0 = l.least[0], q1 = l.least[1], q2 = l.least[2], q3 = l.least[3];
+    const uint32_t quarter = min(min(q0.x, q1.x), min(q2.x, q3.x)), one = max(max(q0.z, q1.z), max(q2.z, q3.z));
+    const uint32_t half = max(max(min(q0.y, q1.y), min(q2.y, q3.y)), min(max(q0.y, q1.y), max(q2.y, q3.y)));   // the second largest
+    return max(max(quarter, half), max(one, 1u));
 }
 
 // Radix selection among the items it[] of all threads, of which more than k are not 0: the smallest of the k largest.  All threads.
@@ -93,12 +119,8 @@ __device__ inline u64 kth_item(TopLds& l, const u64 (&it)[kTopItems], int k) {
         uint32_t h[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[i] = l.hist[turn][255 - 4 * lane - i];
-        uint32_t sum = h[0] + h[1] + h[2] + h[3], upto = sum;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t o = __shfl_up(upto, d);
-            if (lane >= d) upto += o;
-        }
+        uint32_t sum = h[0] + h[1] + h[2] + h[3];
+        const uint32_t upto = (uint32_t)wave_scan((int)sum);
         const int who = __ffsll(__ballot(upto >= (uint32_t)need)) - 1;   // there is one: the bins hold at least `need` items
         uint32_t before = upto - sum, bin = 0, size = 0;
 #pragma unroll
@@ -128,30 +150,23 @@ __device__ inline int keep_from(TopLds& l, const u64 (&it)[kTopItems], u64 least
     return l.count;
 }
 
-// Drops from a list of n <= 256 items those that k others exceed in value, so that at least k are left; the k-th largest value's image where
-// there are k, else 1.  All threads, after a barrier; n becomes the number left, known after one more barrier.
-__device__ inline uint32_t tighten_list(TopLds& l, int n, int k) {
-    const int t = threadIdx.x, w = t >> 6;
-    const u64 it = t < n ? l.list[t] : 0;
-    const uint32_t mine = (uint32_t)(it >> 32);
-    l.maxima[t] = mine;
-    __syncthreads();
-    uint32_t least = ~0u;
-    if (64 * w < n) {   // waves that have items
-        int above = 0;
-#pragma unroll 4
-        for (int i = 0; i < n; i += 4) {
-            const uint4 o = *reinterpret_cast<const uint4*>(&l.maxima[i]);
-            above += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
-        }
-        least = ~wave_max_u32(mine != 0 && above < k ? ~mine : 0u);
+// The bin in which the k-th largest of the counted entries lies.  Every wave for itself: lane x has bins 255 - 4x .. 252 - 4x.
+__device__ inline int kth_bin(const TopLds& l, int k) {
+    const int lane = threadIdx.x & 63;
+    const uint4 q = *reinterpret_cast<const uint4*>(&l.bins[252 - 4 * lane]);
+    const uint32_t h[4] = {q.w, q.z, q.y, q.x};
+    const uint32_t sum = (h[0] + h[1]) + (h[2] + h[3]);
+    const uint32_t upto = (uint32_t)wave_scan((int)sum);
+    const uint64_t enough = __ballot(upto >= (uint32_t)k);
+    if (enough == 0) return 0;
+    uint32_t before = upto - sum;
+    int bin = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (before < (uint32_t)k && before + h[i] >= (uint32_t)k) bin = 255 - 4 * lane - i;
+        before += h[i];
     }
-    if ((t & 63) == 0) l.least[w] = least;
-    if (t == 0) l.count = 0;
-    __syncthreads();
-    least = n < k ? 1u : min(min(l.least[0], l.least[1]), min(l.least[2], l.least[3]));
-    if (mine >= least) l.list[atomicAdd(&l.count, 1)] = it;
-    return least;
+    return __shfl(bin, __builtin_ctzll(enough));
 }
 
 // Brings the list's n <= 256 items into descending order and drops those behind the k-th; how many are left.  All threads.
@@ -173,6 +188,16 @@ __device__ inline int sort_list(TopLds& l, int n, int k) {
     if (t == 0) l.count = min(n, k);
     __syncthreads();
     return min(n, k);
+}
+
+// Frees a list of n <= kTopList items of those whose image is below `least`; how many are left.  All threads, n uniform, after a barrier.
+__device__ inline int thin_list(TopLds& l, int n, uint32_t least) {
+    const int t = threadIdx.x;
+    u64 it[kTopItems];
+#pragma unroll
+    for (int i = 0; i < kTopItems; ++i) it[i] = t + kTopThreads * i < n ? l.list[t + kTopThreads * i] : 0;
+    __syncthreads();
+    return keep_from(l, it, (u64)least << 32);
 }
 
 // Cuts a list of n <= kTopList items to its k largest, in descending order; how many there are.  All threads, n uniform, after a barrier.
@@ -226,6 +251,7 @@ __global__ __launch_bounds__(kTopThreads, 4) void top_segment(const TopArgs a) {
     const typename R::T* p = (const typename R::T*)a.in + (long long)row * a.stride;
     const int v0 = seg * a.seg_len, v1 = min(a.V, v0 + a.seg_len);
     if (t == 0) l.count = 0;
+    l.bins[t] = 0;
     const raw16 none = none16<BF16>();
     auto load = [&](int b, raw16 (&r)[VEC]) {
         if (b + kTopBlock <= v1) {
@@ -241,16 +267,20 @@ __global__ __launch_bounds__(kTopThreads, 4) void top_segment(const TopArgs a) {
     };
     float2 sum = make_float2(kNoEntry, 0.f);
     float from = kNoEntry;   // candidates are not below this: the lowest finite value shuts out -inf (and NaN)
-    int n = 0, next_cut = 2;
-    int done = 0;
+    uint32_t least = 0;      // an image that k of the list's items reach, if it has so many (an exact cut leaves it below `from`)
+    float base = kNoEntry, scale = 0.f;   // bins: (z - base) scale
+    int n = 0, n_known = 0, done = 0;
     // One block, then the load of the one after the next into the same registers: moving a block over would wait for it.  True: the last one.
     auto step = [&](raw16 (&r)[VEC]) {
         const int b = v0 + done * kTopBlock;
         const bool last = b + kTopBlock >= v1;
         ++done;
-        float mx = kNoEntry;
+        float vm[VEC], mx = kNoEntry;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) mx = vec_max<BF16>(r[i], mx);
+        for (int i = 0; i < VEC; ++i) {
+            vm[i] = vec_max<BF16>(r[i], kNoEntry);
+            mx = fmaxf(mx, vm[i]);
+        }
         if (a.lse) {
             const float m = fmaxf(sum.x, mx);
             float s = sum.y * fast_exp2((sum.x - m) * a.c2);
@@ -261,34 +291,63 @@ __global__ __launch_bounds__(kTopThreads, 4) void top_segment(const TopArgs a) {
         if (done == 1) {
             // a thread without an entry above the lowest value counts as one without an entry: the bound only has to be reached by k others
             const uint32_t bound = reached_by(l, mx > kNoEntry ? rank_of(mx) : 0, a.k);
-            if (bound > 1) from = value_of(bound);
+            if (bound > 1) {
+                base = from = value_of(bound);
+                least = bound;
+                const float width = value_of(max(max(l.least[0].w, l.least[1].w), max(l.least[2].w, l.least[3].w))) - base;
+                scale = width > 1e-30f ? 255.f / width : 0.f;
+            }
         }
-        if (mx >= from) {   // one place in the list per thread and block, whatever it brings
+        if (__ballot(mx >= from)) {   // a wave takes its places in the list at once; vectors that bring nothing to any lane are passed over
+            bool some[VEC];
             int brings = 0;
 #pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                some[i] = __ballot(vm[i] >= from) != 0;
+                if (some[i]) {
+#pragma unroll
+                    for (int x = 0; x < N; ++x) brings += R::get(r[i], x) >= from;
+                }
+            }
+            const int upto = wave_scan(brings);
+            int at = 0;
+            if (lane == 63) at = atomicAdd(&l.count, upto);
+            at = __builtin_amdgcn_readlane(at, 63) + upto - brings;
+#pragma unroll
             for (int i = 0; i < VEC; ++i)
+                if (some[i]) {
 #pragma unroll
-                for (int x = 0; x < N; ++x) brings += R::get(r[i], x) >= from;
-            int at = atomicAdd(&l.count, brings);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i)
-#pragma unroll
-                for (int x = 0; x < N; ++x) {
-                    const float z = R::get(r[i], x);
-                    if (z >= from) l.list[at++] = item_of(z, b + N * (t + kTopThreads * i) + x);
+                    for (int x = 0; x < N; ++x) {
+                        const float z = R::get(r[i], x);
+                        if (z >= from) {
+                            l.list[at++] = item_of(z, b + N * (t + kTopThreads * i) + x);
+                            if (scale > 0.f) atomicAdd(&l.bins[min((int)((z - base) * scale), 255)], 1u);
+                        }
+                    }
                 }
         }
         if (b + 2 * kTopBlock < v1) load(b + 2 * kTopBlock, r);
         __syncthreads();
         n = l.count;
-        if (last || n > kTopLow) {
-            n = cut_list(l, n, a.k);
-            if (n == a.k) from = value_of((uint32_t)(l.list[a.k - 1] >> 32) + 1u);
-        } else if (n > a.k && done >= next_cut) {
-            const uint32_t kth = tighten_list(l, n, a.k);
-            if (kth > 1) from = value_of(kth + 1u);
+        if (scale > 0.f && n >= a.k && (last ? n > kTopThreads : n >= n_known + 32)) {
+            // a few units in the last place below the bin's edge: no counted entry of the bin may lie below it
+            const float edge = base + (float)kth_bin(l, a.k) / scale;
+            const float under = edge - 1e-6f * (fabsf(edge) + fabsf(base));
+            from = fmaxf(from, under);
+            least = max(least, rank_of(under));
+            n_known = n;
         }
-        if (done >= next_cut) next_cut = 2 * done;
+        if (last || n > kTopLow) {
+            if (n > kTopThreads) n = n_known = thin_list(l, n, least);
+            if (last || n > kTopThreads) {
+                __syncthreads();   // the count has been read
+                n = n_known = cut_list(l, n, a.k);
+                if (n == a.k) {
+                    least = (uint32_t)(l.list[a.k - 1] >> 32);
+                    from = value_of(least + 1u);
+                }
+            }
+        }
         __syncthreads();   // the count has been read by all before the next block adds to it
         return last;
     };
