@@ -44,7 +44,7 @@ struct DistillArgs {
 
 // What the workgroup keeps of a record: a thread of the first four waves ("place threads") has a place
 struct PlaceLds {
-    int2 list[kPlaces];                  // (token, place) of places that share 16 bytes of the row (or look as if)
+    int2 list[kPlaces + 8];              // (token, place) of places that share 16 bytes of the row (or look as if), then kNowhere
     int n_list, n_found;
     float es[kPlaces];                   // student: 2^((z - z_max) c2), 0 where the place does not count
     float p[kPlaces];                    // teacher: probability times p_sum
@@ -105,6 +105,14 @@ __device__ inline double log_share(float x, float y) {
 // whether another was there before; those that find one stand in a list, and so, a barrier later, does the place whose bit they found.  Only the
 // list is searched, so that the usual row, whose tokens lie far apart, costs one atomic per place.  The outcome does not depend on who came first.
 // Tokens of the same 16 bytes differ in the bits below N only; places that merely share a bit of the table drop out by their tokens.
+constexpr int kNowhere = 1 << 30;   // differs from every token by more than N
+// all threads, before a barrier
+__device__ inline void place_clear(PlaceLds& l) {
+    const int t = threadIdx.x;
+    if (t < kPlaces) l.list[t] = make_int2(kNowhere, kPlaces);
+    if (t < 8) l.list[kPlaces + t] = make_int2(kNowhere, kPlaces);
+    if (t == 0) l.n_list = l.n_found = 0;
+}
 template <typename W>
 __device__ inline bool place_enter(PlaceLds& l, int id, W* word, W bit) {
     if (!bit || !(atomicOr(word, bit) & bit)) return false;
@@ -117,16 +125,16 @@ __device__ inline uint32_t place_flags(PlaceLds& l, int id, bool entered, bool l
     const int t = threadIdx.x, n = l.n_list;
     uint32_t flags = entered ? kHere | kOwner | 1u << (id & (N - 1)) : 0u;
     if (n == 0) return flags;
-    const int none = id ^ (1 << 30);   // (differs from id by far more than N)
     bool meets = false;
     if (entered && !listed)
         for (int i = 0; i < n; i += 8) {   // eight at a time: their reads need not wait for each other
             int o[8];
 #pragma unroll
-            for (int y = 0; y < 8; ++y) o[y] = i + y < n ? l.list[i + y].x : none;
+            for (int y = 0; y < 8; ++y) o[y] = l.list[i + y].x;
 #pragma unroll
             for (int y = 0; y < 8; ++y) meets |= ((uint32_t)o[y] ^ (uint32_t)id) < (uint32_t)N;
         }
+    __syncthreads();   // nobody looks for the list's end any more
     if (meets) l.list[n + atomicAdd(&l.n_found, 1)] = make_int2(id, t);
     __syncthreads();
     if (listed || meets) {
@@ -134,7 +142,7 @@ __device__ inline uint32_t place_flags(PlaceLds& l, int id, bool entered, bool l
         for (int i = 0; i < all; i += 8) {
             int2 o[8];
 #pragma unroll
-            for (int y = 0; y < 8; ++y) o[y] = i + y < all ? l.list[i + y] : make_int2(none, t);
+            for (int y = 0; y < 8; ++y) o[y] = l.list[i + y];
 #pragma unroll
             for (int y = 0; y < 8; ++y) {
                 const uint32_t x = (uint32_t)o[y].x ^ (uint32_t)id;
@@ -142,6 +150,22 @@ __device__ inline uint32_t place_flags(PlaceLds& l, int id, bool entered, bool l
                 flags &= x < (uint32_t)N && o[y].y < t ? (x == 0 ? ~(kHere | kOwner) : ~kOwner) : ~0u;
             }
         }
+    }
+    return flags & kHere ? flags : 0u;
+}
+
+// The same for small vocabularies, where many places share bytes, from the first place of every token (kPlaces: none).
+constexpr int kSmallVocab = 4096;
+template <int N>
+__device__ inline uint32_t place_flags_small(const int* first, int V, int id, bool entered) {
+    if (!entered) return 0;
+    const int t = threadIdx.x, v0 = id & ~(N - 1);
+    uint32_t flags = first[id] == t ? kHere | kOwner : 0u;
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+        const int f = v0 + x < V ? first[v0 + x] : kPlaces;
+        if (f < kPlaces) flags |= 1u << x;
+        if (f < t) flags &= ~kOwner;
     }
     return flags & kHere ? flags : 0u;
 }
@@ -310,7 +334,7 @@ __global__ __launch_bounds__(NT, WAVES) void distill_row(const DistillArgs a) {
         return;
     }
     bits[t] = 0;
-    if (t == 0) l.n_list = l.n_found = 0;
+    place_clear(l);
     __syncthreads();
     // The held vectors live across all phases.  `opaque` makes the compiler take a value as new, so that it neither keeps what an earlier
     // phase derived from it (unpacked elements, addresses, lane masks) nor runs out of registers for it.
@@ -467,6 +491,7 @@ __global__ __launch_bounds__(NT, WAVES) void distill_pass(const DistillArgs a) {
     __shared__ unsigned long long bits[NT];
     __shared__ float2 part[NW];
     __shared__ PlaceLds l;
+    __shared__ int first[kSmallVocab];
     const int t = threadIdx.x, lane = t & 63, row = blockIdx.x;
     const T* p = (const T*)a.in + (long long)row * a.stride;
     T* to = (T*)a.grad + (long long)row * a.grad_stride;
@@ -486,7 +511,10 @@ __global__ __launch_bounds__(NT, WAVES) void distill_pass(const DistillArgs a) {
         return;
     }
     bits[t] = 0;
-    if (t == 0) l.n_list = l.n_found = 0;
+    place_clear(l);
+    const bool small = a.V <= kSmallVocab;
+    if (small)
+        for (int i = t; i < a.V; i += NT) first[i] = kPlaces;
     __syncthreads();
     const uint32_t at = (uint32_t)t * 16u, end_at = (uint32_t)max(whole - 1, 0) * 16u;
     auto load = [&](int i) {   // past the end the last complete vector once more (it is masked out later)
@@ -500,9 +528,13 @@ __global__ __launch_bounds__(NT, WAVES) void distill_pass(const DistillArgs a) {
     for (int i = 0; i < GROUP; ++i) z[i] = load(i);
     const bool entered = id >= 0 && id < a.V;
     bool listed = false;
-    if (t < kPlaces) listed = place_enter(l, id, &bits[(uint32_t)id / N % NT], entered ? 1ull << (id / N / NT) : 0ull);
+    if (small) {
+        if (entered) atomicMin(&first[id], t), atomicOr(&bits[(uint32_t)id / N % NT], 1ull << (id / N / NT));
+    } else if (t < kPlaces) {
+        listed = place_enter(l, id, &bits[(uint32_t)id / N % NT], entered ? 1ull << (id / N / NT) : 0ull);
+    }
     __syncthreads();
-    const uint32_t flags = place_flags<N>(l, id, entered, listed);
+    const uint32_t flags = small ? place_flags_small<N>(first, a.V, id, entered) : place_flags<N>(l, id, entered, listed);
     const bool tail = t == a.k && whole * N < a.V;
     float zp = -INFINITY;
     if (flags & kHere) zp = R::one(p + id);
@@ -667,7 +699,7 @@ __global__ __launch_bounds__(kDisThreads) void distill_grad(const DistillArgs a)
         return;
     }
     table[t] = table[t + kDisThreads] = 0;
-    if (t == 0) l.n_list = l.n_found = 0;
+    place_clear(l);
     __syncthreads();
     int id = -1;
     float value = -INFINITY, zp = -INFINITY;
