@@ -143,9 +143,16 @@ __device__ inline u64 kth_item(TopLds& l, const u64 (&it)[kTopItems], int k) {
 __device__ inline int keep_from(TopLds& l, const u64 (&it)[kTopItems], u64 least) {
     if (threadIdx.x == 0) l.count = 0;
     __syncthreads();
+    int keeps = 0;
+#pragma unroll
+    for (int i = 0; i < kTopItems; ++i) keeps += it[i] != 0 && it[i] >= least;
+    const int upto = wave_scan(keeps);
+    int at = 0;
+    if ((threadIdx.x & 63) == 63) at = atomicAdd(&l.count, upto);
+    at = __builtin_amdgcn_readlane(at, 63) + upto - keeps;
 #pragma unroll
     for (int i = 0; i < kTopItems; ++i)
-        if (it[i] != 0 && it[i] >= least) l.list[atomicAdd(&l.count, 1)] = it[i];
+        if (it[i] != 0 && it[i] >= least) l.list[at++] = it[i];
     __syncthreads();
     return l.count;
 }
@@ -169,19 +176,66 @@ __device__ inline int kth_bin(const TopLds& l, int k) {
     return __shfl(bin, __builtin_ctzll(enough));
 }
 
-// Brings the list's n <= 256 items into descending order and drops those behind the k-th; how many are left.  All threads.
+// The item of lane t ^ S of the wave
+template <int S>
+__device__ inline uint32_t from_lane(uint32_t v) {
+    if constexpr (S == 1) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true);   // quad_perm [1,0,3,2]
+    if constexpr (S == 2) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true);   // quad_perm [2,3,0,1]
+    if constexpr (S == 4) return (uint32_t)__builtin_amdgcn_ds_swizzle((int)v, 0x101F);                    // xor 4
+    if constexpr (S == 8) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, true);  // row_ror:8
+    if constexpr (S == 16) {
+        const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return threadIdx.x & 16 ? p[0] : p[1];
+    }
+    if constexpr (S == 32) {
+        const auto p = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return threadIdx.x & 32 ? p[0] : p[1];
+    }
+}
+// one step of a bitonic network over a workgroup's items, descending in the end; strides of 64 and more go through the list
+template <int SIZE, int STRIDE>
+__device__ inline void bitonic_step(TopLds& l, u64& it) {
+    const int t = threadIdx.x;
+    u64 other;
+    if constexpr (STRIDE >= 64) {
+        __syncthreads();
+        l.list[t] = it;
+        __syncthreads();
+        other = l.list[t ^ STRIDE];
+    } else {
+        other = (u64)from_lane<STRIDE>((uint32_t)(it >> 32)) << 32 | from_lane<STRIDE>((uint32_t)it);
+    }
+    const bool larger = ((t & STRIDE) == 0) == ((t & SIZE) == 0);
+    it = (other > it) == larger ? other : it;
+    if constexpr (STRIDE > 1) bitonic_step<SIZE, STRIDE / 2>(l, it);
+}
+template <int SIZE>
+__device__ inline void bitonic_sort(TopLds& l, u64& it) {
+    if constexpr (SIZE > 2) bitonic_sort<SIZE / 2>(l, it);
+    bitonic_step<SIZE, SIZE / 2>(l, it);
+}
+
+// Brings the list's n <= 256 items into descending order and drops those behind the k-th; how many are left.  All threads.  A few items by
+// counting the larger ones of each (7 n instructions a wave that has some), more by a bitonic network (about 400) where NET: its straight run pays
+// once many workgroups have brought it into the instruction cache (a launch of one workgroup with 240 items: 8.3 us counting, 15.5 us)
+template <bool NET>
 __device__ inline int sort_list(TopLds& l, int n, int k) {
     const int t = threadIdx.x;
-    const u64 mine = t < n ? l.list[t] : 0;
-    if (t == n && (n & 1)) l.list[n] = 0;   // pairs
-    __syncthreads();
-    int at = 0;
-    if ((t & ~63) < n) {   // waves that have items
+    u64 mine = t < n ? l.list[t] : 0;
+    int at = t;
+    if (!NET || n <= 64) {
+        if (t == n && (n & 1)) l.list[n] = 0;   // pairs
+        __syncthreads();
+        if ((t & ~63) < n) {   // waves that have items
+            at = 0;
 #pragma unroll 4
-        for (int i = 0; i < n; i += 2) {
-            const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&l.list[i]);
-            at += (o.x > mine) + (o.y > mine);
+            for (int i = 0; i < n; i += 2) {
+                const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&l.list[i]);
+                at += (o.x > mine) + (o.y > mine);
+            }
         }
+    } else if constexpr (NET) {
+        bitonic_sort<256>(l, mine);
     }
     __syncthreads();
     if (t < n && at < k) l.list[at] = mine;
@@ -200,23 +254,51 @@ __device__ inline int thin_list(TopLds& l, int n, uint32_t least) {
     return keep_from(l, it, (u64)least << 32);
 }
 
-// Cuts a list of n <= kTopList items to its k largest, in descending order; how many there are.  All threads, n uniform, after a barrier.
+// The lower edge of bin `bin`, or a few units in the last place less: no entry counted in it may lie below
+__device__ inline float edge_of(float base, float scale, int bin) {
+    const float edge = base + (float)bin / scale;
+    return edge - 1e-6f * (fabsf(edge) + fabsf(base));
+}
+__device__ inline int bin_of(float z, float base, float scale) { return min((int)((z - base) * scale), 255); }   // z >= base
+__device__ inline float bin_scale(const TopLds& l, float base) {   // after reached_by: 256 bins up to the largest, 0 where there is nothing to tell apart
+    const float width = value_of(max(max(l.least[0].w, l.least[1].w), max(l.least[2].w, l.least[3].w))) - base;
+    return width > 1e-30f ? 255.f / width : 0.f;
+}
+
+// Puts the k largest of the items it[] into the list, in descending order; how many there are.  All threads, after a barrier behind the last use of
+// the list and the bins.
+template <bool NET>
+__device__ inline int cut_items(TopLds& l, const u64 (&it)[kTopItems], int k) {
+    uint32_t mx = 0;
+#pragma unroll
+    for (int i = 0; i < kTopItems; ++i) mx = max(mx, (uint32_t)(it[i] >> 32));
+    const uint32_t bound = reached_by(l, mx, k);
+    l.bins[threadIdx.x] = 0;
+    int n = keep_from(l, it, (u64)bound << 32);
+    const float base = value_of(bound), scale = bound > 1 ? bin_scale(l, base) : 0.f;
+    if (n > kTopThreads && scale > 0.f) {
+#pragma unroll
+        for (int i = 0; i < kTopItems; ++i)
+            if ((uint32_t)(it[i] >> 32) >= bound) atomicAdd(&l.bins[bin_of(value_of((uint32_t)(it[i] >> 32)), base, scale)], 1u);
+        __syncthreads();
+        n = keep_from(l, it, (u64)max(bound, rank_of(edge_of(base, scale, kth_bin(l, k)))) << 32);
+    }
+    if (n > kTopThreads) {
+        __syncthreads();   // the count has been read
+        n = keep_from(l, it, kth_item(l, it, k));
+    }
+    return sort_list<NET>(l, n, k);
+}
+
+// Cuts a list of n <= kTopList items in the same way.  All threads, n uniform, after a barrier; spoils the bins.
+template <bool NET>
 __device__ inline int cut_list(TopLds& l, int n, int k) {
     const int t = threadIdx.x;
-    if (n > kTopThreads) {
-        u64 it[kTopItems], mx = 0;
+    if (n <= kTopThreads) return sort_list<NET>(l, n, k);
+    u64 it[kTopItems];
 #pragma unroll
-        for (int i = 0; i < kTopItems; ++i) {
-            it[i] = t + kTopThreads * i < n ? l.list[t + kTopThreads * i] : 0;
-            mx = max(mx, it[i]);
-        }
-        n = keep_from(l, it, (u64)reached_by(l, (uint32_t)(mx >> 32), k) << 32);
-        if (n > kTopThreads) {
-            __syncthreads();   // the count has been read
-            n = keep_from(l, it, kth_item(l, it, k));
-        }
-    }
-    return sort_list(l, n, k);
+    for (int i = 0; i < kTopItems; ++i) it[i] = t + kTopThreads * i < n ? l.list[t + kTopThreads * i] : 0;
+    return cut_items<NET>(l, it, k);
 }
 
 // The list, sorted, into one row of the outputs
@@ -233,12 +315,12 @@ __device__ inline float lse_of(float2 p, float inv_temp) { return p.y > 0.f ? (f
 struct TopArgs {
     const void* in;
     long long stride;
-    int V, k, segs, seg_len;
+    int V, k, segs, seg_len, slots;   // slots: places for the candidates of a segment, k or more
     float inv_temp, c2;  // c2: logit -> base-2 exponent
     float* values;
     int32_t* ids;
     float* lse;          // may be null
-    u64* lists;          // [rows][segs][k], several segments only
+    u64* lists;          // [rows][segs][slots], several segments only
     float2* parts;       // [rows][segs]
 };
 
@@ -294,8 +376,7 @@ __global__ __launch_bounds__(kTopThreads, 4) void top_segment(const TopArgs a) {
             if (bound > 1) {
                 base = from = value_of(bound);
                 least = bound;
-                const float width = value_of(max(max(l.least[0].w, l.least[1].w), max(l.least[2].w, l.least[3].w))) - base;
-                scale = width > 1e-30f ? 255.f / width : 0.f;
+                scale = bin_scale(l, base);
             }
         }
         if (__ballot(mx >= from)) {   // a wave takes its places in the list at once; vectors that bring nothing to any lane are passed over
@@ -321,7 +402,7 @@ __global__ __launch_bounds__(kTopThreads, 4) void top_segment(const TopArgs a) {
                         const float z = R::get(r[i], x);
                         if (z >= from) {
                             l.list[at++] = item_of(z, b + N * (t + kTopThreads * i) + x);
-                            if (scale > 0.f) atomicAdd(&l.bins[min((int)((z - base) * scale), 255)], 1u);
+                            if (scale > 0.f) atomicAdd(&l.bins[bin_of(z, base, scale)], 1u);
                         }
                     }
                 }
@@ -330,18 +411,17 @@ __global__ __launch_bounds__(kTopThreads, 4) void top_segment(const TopArgs a) {
         __syncthreads();
         n = l.count;
         if (scale > 0.f && n >= a.k && (last ? n > kTopThreads : n >= n_known + 32)) {
-            // a few units in the last place below the bin's edge: no counted entry of the bin may lie below it
-            const float edge = base + (float)kth_bin(l, a.k) / scale;
-            const float under = edge - 1e-6f * (fabsf(edge) + fabsf(base));
-            from = fmaxf(from, under);
-            least = max(least, rank_of(under));
+            const float edge = edge_of(base, scale, kth_bin(l, a.k));
+            from = fmaxf(from, edge);
+            least = max(least, rank_of(edge));
             n_known = n;
         }
         if (last || n > kTopLow) {
             if (n > kTopThreads) n = n_known = thin_list(l, n, least);
-            if (last || n > kTopThreads) {
+            if (n > kTopThreads || (last && n > a.slots)) {
                 __syncthreads();   // the count has been read
-                n = n_known = cut_list(l, n, a.k);
+                if (n > kTopThreads) scale = 0.f;   // bins that cannot tell values apart have done their part
+                n = n_known = cut_list<true>(l, n, a.k);
                 if (n == a.k) {
                     least = (uint32_t)(l.list[a.k - 1] >> 32);
                     from = value_of(least + 1u);
@@ -368,8 +448,8 @@ __global__ __launch_bounds__(kTopThreads, 4) void top_segment(const TopArgs a) {
         }
     }
     if (a.segs > 1) {
-        u64* to = a.lists + ((long long)row * a.segs + seg) * a.k;
-        if (t < a.k) to[t] = t < n ? l.list[t] : 0;
+        u64* to = a.lists + ((long long)row * a.segs + seg) * a.slots;
+        if (t < a.slots) to[t] = t < n ? l.list[t] : 0;
     } else {
         put_list(l, n, a.k, a.values + (long long)row * a.k, a.ids + (long long)row * a.k);
     }
@@ -378,23 +458,17 @@ __global__ __launch_bounds__(kTopThreads, 4) void top_segment(const TopArgs a) {
 // one workgroup per row: the lists of its segments (their unused places are 0)
 __global__ __launch_bounds__(kTopThreads) void top_merge(const TopArgs a) {
     __shared__ TopLds l;
-    const int t = threadIdx.x, lane = t & 63, row = blockIdx.x, all = a.segs * a.k;
+    const int t = threadIdx.x, lane = t & 63, row = blockIdx.x, all = a.segs * a.slots;
     const u64* from = a.lists + (long long)row * all;
-    u64 it[kTopItems], mx = 0;
+    // a run of places for every thread: the unused ones lie at the ends of the lists, and a thread that has none but them has no maximum
+    const int per = (all + kTopThreads - 1) / kTopThreads;
+    u64 it[kTopItems];
 #pragma unroll
-    for (int i = 0; i < kTopItems; ++i) {
-        it[i] = t + kTopThreads * i < all ? from[t + kTopThreads * i] : 0;
-        mx = max(mx, it[i]);
-    }
+    for (int i = 0; i < kTopItems; ++i) it[i] = i < per && per * t + i < all ? from[per * t + i] : 0;
     float2 q = make_float2(kNoEntry, 0.f);
     if (a.lse && t < 64)
         for (int i = lane; i < a.segs; i += 64) q = join_sums(q, a.parts[(long long)row * a.segs + i], a.c2);
-    int n = keep_from(l, it, (u64)reached_by(l, (uint32_t)(mx >> 32), a.k) << 32);
-    if (n > kTopThreads) {
-        __syncthreads();
-        n = keep_from(l, it, kth_item(l, it, a.k));
-    }
-    n = sort_list(l, n, a.k);
+    const int n = cut_items<false>(l, it, a.k);
     put_list(l, n, a.k, a.values + (long long)row * a.k, a.ids + (long long)row * a.k);
     if (a.lse && t < 64) {
         const float m = wave_max_dpp(q.x);
@@ -405,11 +479,12 @@ __global__ __launch_bounds__(kTopThreads) void top_merge(const TopArgs a) {
 
 // Segments of a row: as many as make the call shortest, counted in blocks that pass one after the other.  1024 workgroups are on the chip at
 // once; a workgroup's start and its last cut take as long as one and a half blocks, the merging launch as long as three.
+static int top_slots(int k) { return k + k / 4 + 32 < kTopThreads ? k + k / 4 + 32 : kTopThreads; }   // what the first threshold lets in, usually
 static int top_segs(int n_rows, int vocab, int k) {
     const int blocks = (vocab + kTopBlock - 1) / kTopBlock;
     int best = 1;
     double least = 1e30;
-    for (int segs = 1; segs <= blocks && segs <= kTopList / k && segs <= 64; ++segs) {
+    for (int segs = 1; segs <= blocks && segs <= kTopList / top_slots(k) && segs <= 64; ++segs) {
         const int len = (blocks + segs - 1) / segs;
         if ((blocks + len - 1) / len != segs) continue;   // the same as fewer
         const double rounds = (double)(((long long)n_rows * segs + 1023) / 1024);
@@ -427,7 +502,7 @@ extern "C" size_t psd_top_logits_workspace_bytes(int32_t n_rows, int32_t vocab, 
     if (n_rows < 1 || n_rows > kMaxRows || vocab < 1 || vocab > kMaxVocab || k < 1 || k > PSD_MAX_TOP || k > vocab) return 0;
     const int segs = top_segs(n_rows, vocab, k);
     if (segs == 1) return 16;
-    return align16((size_t)n_rows * segs * k * sizeof(u64)) + align16((size_t)n_rows * segs * sizeof(float2));
+    return align16((size_t)n_rows * segs * top_slots(k) * sizeof(u64)) + align16((size_t)n_rows * segs * sizeof(float2));
 }
 
 extern "C" int psd_top_logits(const void* logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t stride, int32_t k,
@@ -445,10 +520,10 @@ extern "C" int psd_top_logits(const void* logits, int32_t dtype, int32_t n_rows,
     if (workspace_bytes < psd_top_logits_workspace_bytes(n_rows, vocab, k))
         PSD_FAIL(PSD_ENOMEM, err, "%s: workspace %zu < %zu bytes", who, workspace_bytes, psd_top_logits_workspace_bytes(n_rows, vocab, k));
     const int segs = top_segs(n_rows, vocab, k), blocks = (vocab + kTopBlock - 1) / kTopBlock;
-    TopArgs a{logits, stride, vocab, k, segs, (blocks + segs - 1) / segs * kTopBlock, 1.f / temperature, kLog2e / temperature, values, ids, lse, nullptr, nullptr};
+    TopArgs a{logits, stride, vocab, k, segs, (blocks + segs - 1) / segs * kTopBlock, segs > 1 ? top_slots(k) : 0, 1.f / temperature, kLog2e / temperature, values, ids, lse, nullptr, nullptr};
     if (segs > 1) {
         a.lists = (u64*)workspace;
-        a.parts = (float2*)((char*)workspace + align16((size_t)n_rows * segs * k * sizeof(u64)));
+        a.parts = (float2*)((char*)workspace + align16((size_t)n_rows * segs * top_slots(k) * sizeof(u64)));
     }
     hipStream_t st = (hipStream_t)stream;
     if (dtype == PSD_BF16) top_segment<true><<<dim3(segs, n_rows), kTopThreads, 0, st>>>(a);
