@@ -187,15 +187,17 @@ void orc_adjust_row(const float* z, int V, const int32_t* history, int64_t n_his
     free(add);
 }
 
-/* ln sum exp(z / T) over the entries for which skip (may be NULL) is 0; -inf where there is none */
-static double log_sum(const float* z, int V, double T, const unsigned char* skip) {
+/* ln sum exp(z / T - *top) over the entries for which skip (may be NULL) is 0, *top their largest z / T; -inf where there is
+ * none.  The two stay apart: next to a *top of the type's lowest value the logarithm would be lost. */
+static double log_sum(const float* z, int V, double T, const unsigned char* skip, double* top) {
     double m = -INFINITY, s = 0.0;
     for (int v = 0; v < V; ++v)
         if (!(skip && skip[v]) && z[v] / T > m) m = z[v] / T;
+    *top = m;
     if (m == -INFINITY) return m;
     for (int v = 0; v < V; ++v)
         if (!(skip && skip[v])) s += exp(z[v] / T - m);
-    return m + log(s);
+    return log(s);
 }
 
 /* The k largest entries above -inf, descending, equal ones by ascending token; (-inf, -1) in places without one. */
@@ -209,7 +211,9 @@ void orc_top_row(const float* z, int V, int k, double T, double* values, int32_t
         ids[i] = best;
         if (best >= 0) used[best] = 1;
     }
-    *lse = log_sum(z, V, T, NULL);
+    double top;
+    *lse = log_sum(z, V, T, NULL, &top);
+    if (top > -INFINITY) *lse += top;
     free(used);
 }
 
@@ -241,10 +245,11 @@ void orc_distill_row(const float* z, int V, const float* values, const int32_t* 
     p[n] = 0.0;
     if (lse) p[n] = complete || n == V || total >= 1.0 ? 0.0 : 1.0 - total;
     else for (int i = 0; i < n; ++i) p[i] /= total;
-    const double all = log_sum(z, V, T, NULL), rest = log_sum(z, V, T, in_s);
-    double l = 0.0, sum_w = 0.0;
+    double top, rest_top, l = 0.0, sum_w = 0.0;
+    const double all = log_sum(z, V, T, NULL, &top), rest = log_sum(z, V, T, in_s, &rest_top);
+    const double l_rest = rest_top > -INFINITY ? rest_top - top + rest - all : -INFINITY;
     for (int i = 0; i <= n; ++i) {
-        const double lq = (i < n ? z[tok[i]] / T : rest) - all, q = exp(lq);
+        const double lq = i < n ? z[tok[i]] / T - top - all : l_rest, q = exp(lq);
         if (divergence == 0) {
             if (p[i] > 0.0) l += p[i] * (log(p[i]) - lq);
             w[i] = -p[i];
@@ -261,10 +266,10 @@ void orc_distill_row(const float* z, int V, const float* values, const int32_t* 
         /* within the others the derivative spreads by their own distribution */
         for (int v = 0; v < V; ++v)
             if (!in_s[v]) {
-                const double share = z[v] > -INFINITY ? exp(z[v] / T - rest) : 0.0;
-                grad[v] = weight / T * share * (w[n] - exp(rest - all) * sum_w);
+                const double share = z[v] > -INFINITY ? exp(z[v] / T - rest_top - rest) : 0.0;
+                grad[v] = weight / T * share * (w[n] - exp(l_rest) * sum_w);
             }
-        for (int i = 0; i < n; ++i) grad[tok[i]] = weight / T * (w[i] - exp(z[tok[i]] / T - all) * sum_w);
+        for (int i = 0; i < n; ++i) grad[tok[i]] = weight / T * (w[i] - exp(z[tok[i]] / T - top - all) * sum_w);
     }
     free(in_s); free(tok); free(p); free(w);
 }

@@ -145,6 +145,7 @@ def check_adjusted(got, want, size, dtype):
     (1, 32, 8200, [3000], 20, 9, None, 0),               # the widest window
     (2, 11, 32003, [511, 4100], 300, 5, None, 0),
     (1, 2, 128256, [70000], 0, 2, None, 0),              # a long history: counts of thousands
+    (2, 3, 20001, [9000, 14000], 1500, 3, None, 0),      # long histories and long lists of biases
 ])
 def test_adjust_matches_oracle(dtype, S, R, V, lengths, n_bias, n_masks, stride, lead):
     rng = np.random.default_rng(V + S)
@@ -206,6 +207,44 @@ def test_adjust_one_kind_at_a_time_and_none():
         psd.dev_sync()
         assert np.array_equal(y.get(), z, equal_nan=True)
     del keep
+
+
+def test_rows_far_apart():
+    """Rows more than 2^31 elements apart: every offset is taken in 64 bits."""
+    rng = np.random.default_rng(9)
+    n, V, k, stride = 2, 3000, 5, 2 ** 31 + 5
+    t, z = pair(rng, n, V, psd.BF16)
+    z = rounded(z, psd.BF16)
+    buf = psd.DeviceBuffer((stride + V) * 2)
+    L = psd.lib()
+    for r in range(n):
+        bits = to_bf16(z[r])
+        psd.binding._check(L.psd_dev_copy(buf.data_ptr() + r * stride * 2, bits.ctypes.data, bits.nbytes, 0))
+
+    def rows():
+        out = np.empty((n, V), np.uint16)
+        for r in range(n):
+            psd.binding._check(L.psd_dev_copy(out[r].ctypes.data, buf.data_ptr() + r * stride * 2, V * 2, 1))
+        return synth.bf16_to_f32(out)
+
+    got = run_top(buf, n, V, k, 1.0, psd.BF16, stride)
+    check_top(z, k, 1.0, got)
+    values, ids, lse = records(t, k, 1.0)
+    loss, nb = dev(np.zeros(n, np.float32)), psd.distill_workspace_bytes(n, V, k)
+    ws = psd.DeviceBuffer(nb)
+    small = Rows(z * 0, psd.BF16)
+    psd.distill(buf, n, V, dev(values), dev(ids), dev(lse), k, 1.0, psd.DIV_KL, None, loss, small, ws, nb, dtype=psd.BF16, stride=stride)
+    grad = small.get()
+    check_distill(z, values, ids, lse, 1.0, psd.DIV_KL, None, sync_get(loss, np.float32, n), grad, psd.BF16)
+    psd.adjust_logits(buf, buf, 1, n, V, psd.Adjust(bias=dev(np.array([2.0], np.float32)), bias_tokens=dev(np.array([7], np.int32)), bias_offsets=dev(np.array([0, 1], np.int64)), n_bias=1),
+                      dtype=psd.BF16, logits_stride=stride, out_stride=stride)
+    psd.dev_sync()
+    want = z.copy()
+    want[:, 7] = rounded(want[:, 7] + 2, psd.BF16)
+    assert np.array_equal(rows(), want)
+    psd.distill(buf, n, V, dev(values), dev(ids), dev(lse), k, 1.0, psd.DIV_KL, None, loss, buf, ws, nb, dtype=psd.BF16, stride=stride, grad_stride=stride)
+    psd.dev_sync()
+    check_distill(want, values, ids, lse, 1.0, psd.DIV_KL, None, loss.to_numpy(np.float32, n), rows(), psd.BF16)
 
 
 def test_adjust_brings_bad_offsets_into_range():
@@ -324,7 +363,7 @@ def distill_bounds(z, values, ids, lse, T, div, weight):
     V = z.size
     a = z.astype(np.float64) / T
     with np.errstate(divide="ignore", invalid="ignore"):   # -inf logits
-        lq = a - oracle.top_row(z, 1, T)[2]
+        lq = a - a.max() - np.log(np.exp(a - a.max()).sum())   # the largest entry first: it may be the type's lowest value
     q = np.exp(lq)
     seen, first = set(), []
     for i, v in enumerate(ids):
@@ -486,6 +525,36 @@ def test_distill_without_student_mass():
     loss, grad = run_distill(x, 4, V, values, ids, lse, 3, 1.0, psd.DIV_JSD, None, psd.F32)
     assert np.isfinite(loss[:3]).all() and np.isfinite(grad[:3]).all() and np.isnan(loss[3])
     check_distill(z[:3], values[:3], ids[:3], lse[:3], 1.0, psd.DIV_JSD, None, loss[:3], grad[:3], psd.F32)
+
+
+def test_distill_lowest_values_and_tiny_vocabularies():
+    low = -3.402823466e38
+    V, k = 5000, 4
+    z = np.zeros((4, V), np.float32)
+    z[0] = low                                      # the lowest value throughout is a uniform row
+    z[1, 100:] = low                                # a mask of the lowest value
+    z[2] = -1e30
+    z[2, 3] = -2e30
+    z[3] = np.linspace(-3, 3, V)
+    values = np.array([[1, 0.5, 0, low], [2, 1, 0, -1], [1, 1, 1, 1], [0.5, 0.25, -np.inf, 1]], np.float32)
+    ids = np.array([[3, 9, 200, 4999], [0, 99, 100, 5], [3, 4, 5, 6], [4999, 0, 17, 18]], np.int32)
+    for lse in (None, np.array([3.0, 2.5, 3.0, 2.0], np.float32)):
+        for div in (psd.DIV_KL, psd.DIV_JSD):
+            loss, grad = run_distill(Rows(z, psd.F32), 4, V, values, ids, lse, k, 1.0, div, None, psd.F32)
+            kl_inf = div == psd.DIV_KL               # rows 1 and 2 have tokens of the teacher that underflow to no mass at all
+            for r in (0, 3) if kl_inf else range(4):
+                ls = None if lse is None else lse[r:r + 1]
+                check_distill(z[r:r + 1], values[r:r + 1], ids[r:r + 1], ls, 1.0, div, None, loss[r:r + 1], grad[r:r + 1], psd.F32)
+            assert np.isfinite(grad).all() and not np.isnan(loss).any()
+    # a record longer than the vocabulary: repetitions, tokens that are none
+    rng = np.random.default_rng(3)
+    for V in (1, 3, 9):
+        z = rng.normal(0, 1, (2, V)).astype(np.float32)
+        ids = rng.integers(0, V + 2, (2, 200)).astype(np.int32)
+        values = rng.normal(0, 1, (2, 200)).astype(np.float32)
+        for div in (psd.DIV_KL, psd.DIV_JSD):
+            loss, grad = run_distill(Rows(z, psd.F32), 2, V, values, ids, None, 200, 1.0, div, None, psd.F32)
+            check_distill(z, values, ids, None, 1.0, div, None, loss, grad, psd.F32)
 
 
 def test_distill_gradient_is_that_of_differences_of_its_own_loss():

@@ -211,3 +211,11 @@ def test_host_arrays_are_refused():
         psd.top_logits(host, 1, 100, 4, 1.0, A, A, A, A, 1 << 20)
     with pytest.raises(TypeError):
         psd.distill(A, 1, 100, A, A, A, 4, 1.0, psd.DIV_KL, None, A, host, A, 1 << 20)
+
+
+def test_adjust_struct_has_the_layout_of_the_header():
+    import ctypes
+    A = psd.Adjust
+    assert ctypes.sizeof(A) == 14 * 8 and [getattr(A, n).offset for n, _ in A._fields_] == list(range(0, 112, 8))
+    assert [n for n, _ in A._fields_] == ["history", "history_offsets", "n_history", "n_prompt", "window", "window_stride", "penalties", "bias_tokens", "bias",
+                                          "bias_offsets", "n_bias", "masks", "mask_index", "n_masks"]
