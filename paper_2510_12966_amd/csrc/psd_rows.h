@@ -3,6 +3,9 @@
 #include "psd_device.h"
 #include "psd_host.h"
 
+// Every fused multiply-add behind this line is written out: kernels that form the same sum in different surroundings round alike.
+#pragma clang fp contract(off)
+
 namespace psd {
 
 constexpr int kMaxRows = 65535;       // rows of a call, as in psd_sample and psd_row_stats
