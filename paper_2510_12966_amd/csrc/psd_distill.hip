@@ -826,7 +826,7 @@ extern "C" int psd_distill(const void* logits, int32_t dtype, int32_t n_rows, in
         PSD_FAIL(PSD_EINVAL, err, "%s: grad overlaps the logits", who);
     if (!top_values || !top_ids || !loss || !workspace) PSD_FAIL(PSD_EINVAL, err, "%s: null pointer", who);
     if (k < 1 || k > PSD_MAX_TOP) PSD_FAIL(PSD_EINVAL, err, "%s: k=%d", who, k);
-    if (!(temperature > 0.f)) PSD_FAIL(PSD_EINVAL, err, "%s: temperature=%g", who, temperature);
+    if (!temperature_fits(temperature)) PSD_FAIL(PSD_EINVAL, err, "%s: temperature=%g", who, temperature);
     if (divergence != PSD_DIV_KL && divergence != PSD_DIV_JSD) PSD_FAIL(PSD_EINVAL, err, "%s: divergence=%d", who, divergence);
     if (((uintptr_t)top_values | (uintptr_t)top_ids | (uintptr_t)top_lse | (uintptr_t)row_weights | (uintptr_t)loss) & 3 || ((uintptr_t)workspace & 15))
         PSD_FAIL(PSD_EINVAL, err, "%s: misaligned record, weights, loss or workspace", who);

@@ -118,4 +118,7 @@ inline int rows_check(const char* who, const void* logits, int dtype, long long 
     return PSD_OK;
 }
 
+// exponents are taken as differences times kLog2e / temperature, which has to be a number
+inline bool temperature_fits(float temperature) { return temperature > 0.f && temperature <= 3.402823466e38f && kLog2e / temperature <= 3.402823466e38f; }
+
 }  // namespace psd

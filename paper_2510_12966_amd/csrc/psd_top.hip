@@ -514,7 +514,7 @@ extern "C" int psd_top_logits(const void* logits, int32_t dtype, int32_t n_rows,
     if (rc != PSD_OK) return rc;
     if (!values || !ids || !workspace) PSD_FAIL(PSD_EINVAL, err, "%s: null pointer", who);
     if (k < 1 || k > PSD_MAX_TOP || k > vocab) PSD_FAIL(PSD_EINVAL, err, "%s: k=%d of %d entries", who, k, vocab);
-    if (!(temperature > 0.f)) PSD_FAIL(PSD_EINVAL, err, "%s: temperature=%g", who, temperature);
+    if (!temperature_fits(temperature)) PSD_FAIL(PSD_EINVAL, err, "%s: temperature=%g", who, temperature);
     if (((uintptr_t)values | (uintptr_t)ids | (uintptr_t)lse) & 3 || ((uintptr_t)workspace & 15))
         PSD_FAIL(PSD_EINVAL, err, "%s: misaligned outputs or workspace", who);
     if (workspace_bytes < psd_top_logits_workspace_bytes(n_rows, vocab, k))

@@ -201,6 +201,14 @@ def test_distill_refusals():
         assert psd.distill_workspace_bytes(*args) == 0
 
 
+def test_temperatures_without_a_finite_scale_are_refused():
+    """0 * inf would be the exponent of a row's largest entry, or of an entry of -inf."""
+    n, V, k = 4, 1000, 8
+    for T in (float("inf"), 1e-39, -0.0, -float("inf")):
+        _refused(-1, psd.top_logits, A, n, V, k, T, B, B, None, B, 1 << 20)
+        _refused(-1, psd.distill, A, n, V, B, B, None, k, T, psd.DIV_JSD, None, B, None, B, 1 << 20)
+
+
 def test_host_arrays_are_refused():
     host = np.zeros(100, np.float32)
     with pytest.raises(TypeError):
