@@ -34,9 +34,10 @@ typedef int32_t four_tokens __attribute__((ext_vector_type(4), aligned(4)));
 
 struct Penalty { float repetition, inverse, presence, frequency; };   // inverse: 1 / repetition
 
-// One logit.  The quotient comes from the rounded inverse and one correction by its remainder (exact in the fused multiply-add).
+// One logit.  The quotient comes from the rounded inverse and one correction by its remainder (exact in the fused multiply-add); one beyond
+// the largest float has no remainder and stays infinite.
 __device__ inline float adjusted(float z, uint32_t count, const Penalty& p) {
-    const float q = z * p.inverse, quotient = __builtin_amdgcn_div_fixupf(fmaf(fmaf(-q, p.repetition, z), p.inverse, q), p.repetition, z);
+    const float q = z * p.inverse, corrected = fmaf(fmaf(-q, p.repetition, z), p.inverse, q), quotient = corrected == corrected ? corrected : q;
     const float y = z > 0.f ? quotient : z * p.repetition;
     const uint32_t occurrences = count & ~kPromptOnly;
     const float minus = occurrences ? fmaf((float)occurrences, p.frequency, p.presence) : 0.f;
