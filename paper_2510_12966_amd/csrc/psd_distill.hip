@@ -51,6 +51,7 @@ struct PlaceLds {
     float z_max[kPlaceWaves], t_max[kPlaceWaves];
     int valid[kPlaceWaves], open[kPlaceWaves];
     double sums[5][kPlaceWaves];
+    float lse;                           // of the teacher's row, 0 where the record is all of it
     float rest, rest_max;                // the others' gradient is rest * 2^((z - rest_max) c2)
     float2 tail;
 };
@@ -186,6 +187,7 @@ __device__ inline void place_second(const DistillArgs& a, PlaceLds& l, uint32_t 
     const float es = flags & kHere ? fast_exp2(x) : 0.f;
     const double lp = a.lse ? (double)value * a.inv_temp - (double)a.lse[row] : ((double)value - (double)max_of(l.t_max)) * a.inv_temp;
     const float p = flags & kHere ? exp_of(lp) : 0.f;
+    if (t == 0) l.lse = a.lse ? a.lse[row] : 0.f;
     l.es[t] = es;
     l.p[t] = p;
     const double d = wave_sum(x_times(p, lp - (double)x * kLn2d));
@@ -215,8 +217,11 @@ __device__ inline RowSums row_sums(const DistillArgs& a, const PlaceLds& l, floa
     const double s = sum_of(l.sums[1]);
     r.p_place = a.lse ? 1.0 : 1.0 / s;
     r.mass = a.lse ? s : 1.0;
-    // a negative token: the teacher has no entries beside those of its record
-    r.p_rest = a.lse && sum_of(l.open) == 0 && sum_of(l.valid) < a.V && s < 1.0 ? 1.0 - s : 0.0;
+    // A negative token: the teacher has no entries beside those of its record.  A record that just holds them all has none, and then 1 - s is
+    // what the roundings leave (lse is a float, off by 2^-24 of itself, its logarithm and the p by a few 2^-24 more): a student that has no
+    // entry beside them either is not held to it, for that would cost it an infinite divergence.
+    const bool noise = tail.y == 0.f && 1.0 - s <= (2.0 + fabs((double)l.lse)) * 0x1p-22;
+    r.p_rest = a.lse && sum_of(l.open) == 0 && sum_of(l.valid) < a.V && s < 1.0 && !noise ? 1.0 - s : 0.0;
     r.scale = (double)weight * a.inv_temp;
     return r;
 }

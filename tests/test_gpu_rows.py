@@ -579,6 +579,29 @@ def test_distill_lowest_values_and_tiny_vocabularies():
             check_distill(z, values, ids, None, 1.0, div, None, loss, grad, psd.F32)
 
 
+def test_distill_a_record_that_just_holds_a_grammars_tokens():
+    """Masks that leave k tokens, recorded with that k: no place says that the record is complete, and the sum of its probabilities is off 1 by roundings."""
+    rng = np.random.default_rng(31)
+    for n, V, k in ((64, 1000, 2), (64, 5000, 7), (300, 5000, 64), (20, 128256, 3)):
+        t, z = pair(rng, n, V, psd.F32, spread=8)
+        allowed = np.argpartition(rng.random((n, V)), k, axis=1)[:, :k]
+        closed = np.ones((n, V), bool)
+        np.put_along_axis(closed, allowed, False, axis=1)
+        t[closed] = z[closed] = -INF
+        values, ids, lse = run_top(Rows(t, psd.F32), n, V, k, 1.0, psd.F32)
+        a, b = (np.take_along_axis(y, ids, 1).astype(np.float64) for y in (t, z))
+        lp, lq = a - np.logaddexp.reduce(a, 1, keepdims=True), b - np.logaddexp.reduce(b, 1, keepdims=True)
+        want = (np.exp(lp) * (lp - lq)).sum(1)
+        loss, grad = run_distill(Rows(z, psd.F32), n, V, values, ids, lse, k, 1.0, psd.DIV_KL, None, psd.F32)
+        # every ln p off by the record's lse and a few roundings more, the remainder left out
+        tol = 2.0 ** -20 * (2 + np.abs(lse)) * (1 + np.abs(lp - lq).max(1))
+        assert (np.abs(loss - want) <= tol).all() and (grad[closed] == 0).all()
+        assert (np.abs(np.take_along_axis(grad, ids, 1) - (np.exp(lq) - np.exp(lp))) <= tol[:, None]).all()
+        # a record with a true remainder: the student has no mass for it
+        loss, _ = run_distill(Rows(z, psd.F32), n, V, values, ids, lse + np.float32(0.01), k, 1.0, psd.DIV_KL, None, psd.F32)
+        assert np.isposinf(loss).all()
+
+
 def test_distill_gradient_is_that_of_differences_of_its_own_loss():
     rng = np.random.default_rng(8)
     V, k, T = 300, 9, 1.0
