@@ -22,10 +22,8 @@ struct AdjustArgs {
     psd_adjust a;
 };
 
-// the part lo .. hi - 1 of a concatenation of n entries that belongs to list s
-__device__ inline void list_of(const int64_t* offsets, int s, int64_t n, int64_t& lo, int64_t& hi) {
-    lo = offsets[s];
-    hi = offsets[s + 1];
+// the part lo .. hi - 1 of a concatenation of n entries that belongs to a list with these offsets
+__device__ inline void clamp_list(int64_t& lo, int64_t& hi, int64_t n) {
     lo = lo < 0 ? 0 : lo > n ? n : lo;
     hi = hi < lo ? lo : hi > n ? n : hi;
 }
@@ -44,25 +42,26 @@ __device__ inline float adjusted(float z, uint32_t count, const Penalty& p) {
     return count ? y - minus : z;
 }
 
+// Where a sequence's lists lie.  Asked for all together, before anything waits.
+struct Lists {
+    int64_t lo, hi, counted, b0, b1;   // history, the first of its tokens that count, biases
+    int m0, m1, m2;                    // the masks of the group's first rows
+};
+
 // What the lists say about the n entries from v0 on: occurrences in the history and in the window's first j0 tokens, and biases.  All threads,
 // after the counts and biases have been cleared; a barrier at its end.
 template <int NT>
-__device__ inline void read_lists(const AdjustArgs& g, uint32_t* count, uint32_t* bias, const int32_t* window, int s, int v0, int n, int j0) {
+__device__ inline void read_lists(const AdjustArgs& g, const Lists& w, uint32_t* count, uint32_t* bias, const int32_t* window, int v0, int n, int j0) {
     constexpr int AHEAD = 4;
     const psd_adjust& a = g.a;
     const int t = threadIdx.x;
     // the first of the biases (all of them, most of the time) set out first
-    int64_t b0 = 0, b1 = 0;
+    const int64_t b0 = w.b0, b1 = w.b1;
     int32_t btok = -1;
     float bval = 0.f;
-    if (a.bias) {
-        list_of(a.bias_offsets, s, a.n_bias, b0, b1);
-        if (b0 + t < b1) btok = a.bias_tokens[b0 + t], bval = a.bias[b0 + t];
-    }
-    if (a.history) {
-        int64_t lo, hi;
-        list_of(a.history_offsets, s, a.n_history, lo, hi);
-        const int64_t counted = lo + (a.n_prompt ? max(0, a.n_prompt[s]) : 0);
+    if (b0 + t < b1) btok = a.bias_tokens[b0 + t], bval = a.bias[b0 + t];
+    {
+        const int64_t lo = w.lo, hi = w.hi, counted = w.counted;
         for (int64_t i0 = lo; i0 < hi; i0 += 4 * NT * AHEAD) {
             int32_t tok[AHEAD][4];
 #pragma unroll
@@ -118,7 +117,7 @@ __device__ inline void read_lists(const AdjustArgs& g, uint32_t* count, uint32_t
 // The rows j0 .. j1 - 1 of a chunk: WHOLE where it lies inside the vocabulary.  Two rows are on their way while one is written; their registers
 // take turns (moving a row over would wait for it).
 template <bool BF16, int NT, bool WHOLE>
-__device__ inline void adjust_group(const AdjustArgs& g, uint32_t* count, uint32_t* bias, const Penalty& pen, int s, int v0, int j0, int j1) {
+__device__ inline void adjust_group(const AdjustArgs& g, const Lists& lists, uint32_t* count, uint32_t* bias, const Penalty& pen, int s, int v0, int j0, int j1) {
     typedef Row<BF16> R;
     typedef typename R::T T;
     constexpr int N = R::N, VEC = kAdjPer / N;
@@ -142,18 +141,18 @@ __device__ inline void adjust_group(const AdjustArgs& g, uint32_t* count, uint32
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
                 const int u = N * (t + NT * i);
-                if (WHOLE || u < n) open[i] = mask[u >> 5] >> (u & 31);
+                if (WHOLE || u < n) open[i] = mask[u >> 5];   // shifted at its use, which waits for it
             }
         }
     };
     raw16 even[VEC], odd[VEC];
     uint32_t open_even[VEC], open_odd[VEC];
-    int j = j0, m_next = mask_of(j0 + 2);
-    load(j0, mask_of(j0), even, open_even);
-    if (j0 + 1 < j1) load(j0 + 1, mask_of(j0 + 1), odd, open_odd);
+    int j = j0, m_next = lists.m2;
+    load(j0, lists.m0, even, open_even);
+    if (j0 + 1 < j1) load(j0 + 1, lists.m1, odd, open_odd);
     const int32_t* window = a.window ? a.window + (int64_t)s * a.window_stride : nullptr;
     __syncthreads();
-    read_lists<NT>(g, count, bias, window, s, v0, n, j0);
+    read_lists<NT>(g, lists, count, bias, window, v0, n, j0);
     auto step = [&](raw16 (&z)[VEC], uint32_t (&open)[VEC]) {   // true: the last row
         T* to = (T*)g.out + (row0 + j) * g.out_stride + v0;
 #pragma unroll
@@ -182,8 +181,9 @@ __device__ inline void adjust_group(const AdjustArgs& g, uint32_t* count, uint32
                     e[q + 3] += b.w;
                 }
             }
+            const uint32_t allowed = open[i] >> (u & 31);
 #pragma unroll
-            for (int x = 0; x < N; ++x) e[x] = (open[i] >> x) & 1 ? e[x] : -INFINITY;
+            for (int x = 0; x < N; ++x) e[x] = (allowed >> x) & 1 ? e[x] : -INFINITY;
             if (WHOLE) __builtin_nontemporal_store((typename R::V)R::pack(e), (typename R::V*)(to + u));
             else if (u < n) row_store<BF16>(to, u, n, e);
         }
@@ -214,15 +214,30 @@ __global__ __launch_bounds__(NT, 4) void adjust_rows(const AdjustArgs g) {
     uint32_t* const bias = count + (g.counts ? CHUNK : 0);   // places in the list (from 1 on), then the biases themselves
     // the sequence is the fastest index: workgroups go round the dies, and the chunks of one sequence read its history out of the same L2
     const int s = blockIdx.x, v0 = blockIdx.z * CHUNK, j0 = blockIdx.y * g.group, j1 = min(g.rows, j0 + g.group);
+    // What there is of each list is looked up by loads that no branch keeps from setting out together: those of an absent list read the
+    // arguments themselves.
+    const psd_adjust& a = g.a;
+    const uint64_t here = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+    const auto* off = (const __attribute__((address_space(4))) int64_t*)(a.history ? (uint64_t)(a.history_offsets + s) : here);
+    const auto* boff = (const __attribute__((address_space(4))) int64_t*)(a.bias ? (uint64_t)(a.bias_offsets + s) : here);
+    const auto* prompt = (const __attribute__((address_space(4))) int32_t*)(a.n_prompt ? (uint64_t)(a.n_prompt + s) : here);
+    const auto* mask = (const __attribute__((address_space(4))) int32_t*)(a.mask_index ? (uint64_t)(a.mask_index + (long long)s * g.rows + j0) : here);
+    const auto* pens = (const __attribute__((address_space(4))) float*)(a.penalties ? (uint64_t)(a.penalties + 3 * (int64_t)s) : here);
+    const int more = a.mask_index ? j1 - 1 - j0 : 0;
+    Lists lists{off[0], off[1], prompt[0], boff[0], boff[1], mask[0], mask[min(1, more)], mask[min(2, more)]};
+    Penalty pen{pens[0], 0.f, pens[1], pens[2]};
     for (int i = threadIdx.x; i < (g.counts + g.biases) * (CHUNK / 4); i += NT) lds[i] = make_uint4(0, 0, 0, 0);
-    Penalty pen{1.f, 1.f, 0.f, 0.f};
-    if (g.a.penalties) {
-        const float* p = g.a.penalties + 3 * (int64_t)s;
-        const float r = p[0] > 0.f ? p[0] : 1.f;
-        pen = Penalty{r, 1.f / r, p[1], p[2]};
-    }
-    if (v0 + CHUNK <= g.V) adjust_group<BF16, NT, true>(g, count, bias, pen, s, v0, j0, j1);
-    else adjust_group<BF16, NT, false>(g, count, bias, pen, s, v0, j0, j1);
+    clamp_list(lists.lo, lists.hi, a.n_history);
+    clamp_list(lists.b0, lists.b1, a.n_bias);
+    lists.counted = a.n_prompt ? lists.lo + max((int64_t)0, lists.counted) : lists.lo;
+    if (!a.history) lists.hi = lists.lo;
+    if (!a.bias) lists.b1 = lists.b0;
+    if (!a.mask_index) lists.m0 = lists.m1 = lists.m2 = -1;
+    if (!a.penalties) pen = Penalty{1.f, 1.f, 0.f, 0.f};
+    if (!(pen.repetition > 0.f)) pen.repetition = 1.f;
+    pen.inverse = 1.f / pen.repetition;
+    if (v0 + CHUNK <= g.V) adjust_group<BF16, NT, true>(g, lists, count, bias, pen, s, v0, j0, j1);
+    else adjust_group<BF16, NT, false>(g, lists, count, bias, pen, s, v0, j0, j1);
 }
 
 template <bool BF16, int NT>
