@@ -55,36 +55,56 @@ __device__ inline void read_lists(const AdjustArgs& g, const Lists& w, uint32_t*
     constexpr int AHEAD = 4;
     const psd_adjust& a = g.a;
     const int t = threadIdx.x;
+    const uint32_t spare = kAdjPer * NT + (t & 63);
     // the first of the biases (all of them, most of the time) set out first
     const int64_t b0 = w.b0, b1 = w.b1;
     int32_t btok = -1;
     float bval = 0.f;
     if (b0 + t < b1) btok = a.bias_tokens[b0 + t], bval = a.bias[b0 + t];
-    {
-        const int64_t lo = w.lo, hi = w.hi, counted = w.counted;
-        for (int64_t i0 = lo; i0 < hi; i0 += 4 * NT * AHEAD) {
-            int32_t tok[AHEAD][4];
+    if (w.lo < w.hi) {   // two parts of the history on their way, in registers that take turns
+        constexpr int PART = 4 * NT * AHEAD;
+        auto fetch = [&](int32_t (&tok)[AHEAD][4], int64_t i0) {
 #pragma unroll
             for (int x = 0; x < AHEAD; ++x) {
                 const int64_t i = i0 + 4 * (t + NT * x);
-                if (i + 4 <= hi) {
+                if (i + 4 <= w.hi) {
                     const four_tokens f = *reinterpret_cast<const four_tokens*>(a.history + i);
 #pragma unroll
                     for (int y = 0; y < 4; ++y) tok[x][y] = f[y];
                 } else {
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) tok[x][y] = i + y < hi ? a.history[i + y] : -1;
+                    for (int y = 0; y < 4; ++y) tok[x][y] = i + y < w.hi ? a.history[i + y] : -1;
                 }
             }
+        };
+        auto enter = [&](const int32_t (&tok)[AHEAD][4], int64_t i0) {
 #pragma unroll
-            for (int x = 0; x < AHEAD; ++x)
+            for (int x = 0; x < AHEAD; ++x) {
+                // tokens of other chunks add to words behind the table, for a branch costs more than an addition; a wave whose tokens all
+                // count, or none of them, does one of the two
+                if (i0 + 4 * ((t & ~63) + NT * x) >= w.hi) break;
+                const int before = (int)min(max(w.counted - (i0 + 4 * (t + NT * x)), (int64_t)0), (int64_t)4);   // of this thread's tokens
+                uint32_t* at[4];
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const uint32_t u = (uint32_t)tok[x][y] - (uint32_t)v0;
-                    if (u >= (uint32_t)n) continue;
-                    if (i0 + 4 * (t + NT * x) + y >= counted) atomicAdd(&count[u], 1u);
-                    else atomicOr(&count[u], kPromptOnly);
-                }
+                for (int y = 0; y < 4; ++y) at[y] = count + min((uint32_t)tok[x][y] - (uint32_t)v0, spare);
+                if (__ballot(before < 4))
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) atomicAdd(y < before ? count + spare : at[y], 1u);
+                if (__ballot(before > 0))
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) atomicOr(y < before ? at[y] : count + spare, kPromptOnly);
+            }
+        };
+        int32_t even[AHEAD][4], odd[AHEAD][4];
+        fetch(even, w.lo);
+        if (w.lo + PART < w.hi) fetch(odd, w.lo + PART);
+        for (int64_t i0 = w.lo;; i0 += 2 * PART) {
+            enter(even, i0);
+            if (i0 + PART >= w.hi) break;
+            if (i0 + 2 * PART < w.hi) fetch(even, i0 + 2 * PART);
+            enter(odd, i0 + PART);
+            if (i0 + 2 * PART >= w.hi) break;
+            if (i0 + 3 * PART < w.hi) fetch(odd, i0 + 3 * PART);
         }
     }
     if (window)
@@ -211,7 +231,7 @@ __global__ __launch_bounds__(NT, 4) void adjust_rows(const AdjustArgs g) {
     constexpr int CHUNK = kAdjPer * NT;
     extern __shared__ uint4 lds[];
     uint32_t* const count = reinterpret_cast<uint32_t*>(lds);
-    uint32_t* const bias = count + (g.counts ? CHUNK : 0);   // places in the list (from 1 on), then the biases themselves
+    uint32_t* const bias = count + (g.counts ? CHUNK + 64 : 0);   // places in the list (from 1 on), then the biases themselves
     // the sequence is the fastest index: workgroups go round the dies, and the chunks of one sequence read its history out of the same L2
     const int s = blockIdx.x, v0 = blockIdx.z * CHUNK, j0 = blockIdx.y * g.group, j1 = min(g.rows, j0 + g.group);
     // What there is of each list is looked up by loads that no branch keeps from setting out together: those of an absent list read the
@@ -226,7 +246,7 @@ __global__ __launch_bounds__(NT, 4) void adjust_rows(const AdjustArgs g) {
     const int more = a.mask_index ? j1 - 1 - j0 : 0;
     Lists lists{off[0], off[1], prompt[0], boff[0], boff[1], mask[0], mask[min(1, more)], mask[min(2, more)]};
     Penalty pen{pens[0], 0.f, pens[1], pens[2]};
-    for (int i = threadIdx.x; i < (g.counts + g.biases) * (CHUNK / 4); i += NT) lds[i] = make_uint4(0, 0, 0, 0);
+    for (int i = threadIdx.x; i < (g.counts + g.biases) * (CHUNK / 4) + 16 * g.counts; i += NT) lds[i] = make_uint4(0, 0, 0, 0);
     clamp_list(lists.lo, lists.hi, a.n_history);
     clamp_list(lists.b0, lists.b1, a.n_bias);
     lists.counted = a.n_prompt ? lists.lo + max((int64_t)0, lists.counted) : lists.lo;
@@ -244,7 +264,7 @@ template <bool BF16, int NT>
 static void adjust_launch(AdjustArgs& g, int n_seqs, hipStream_t st) {
     const int chunks = (g.V + kAdjPer * NT - 1) / (kAdjPer * NT);
     const dim3 grid(n_seqs, (g.rows + g.group - 1) / g.group, chunks);
-    adjust_rows<BF16, NT><<<grid, NT, (size_t)(g.counts + g.biases) * kAdjPer * NT * 4, st>>>(g);
+    adjust_rows<BF16, NT><<<grid, NT, (size_t)(g.counts + g.biases) * kAdjPer * NT * 4 + 256 * g.counts, st>>>(g);
 }
 
 }  // namespace psd
