@@ -356,8 +356,9 @@ extern "C" int psd_adjust_logits(const void* logits, void* out, int32_t dtype, i
     // 15.2 / 12.1, 30000: 37.8 / 18.7; 9 rows for each of 64: 500 tokens 114.5 / 117.5, 30000: 129.4 / 122.4)
     const long long units = (vocab + 4095LL) / 4096 * n_seqs, tokens = a.history ? a.n_history / n_seqs : 0;
     const bool large = a.history && (tokens > 16384 || (tokens > 4096 && units >= 1024) || (rows == 1 && units >= 2048));
-    // Every group of rows reads the lists again and leaves a workgroup more: groups of one row as long as the chip is not full, larger ones then (us;
-    // 32 rows of 32000 for 8 sequences: 1 / 2 / 5 rows a group 16.1 / 14.6 / 18.9; 9 rows of 128256 for 48: 98 / 93 / 91)
+    // Every group of rows reads the lists again and leaves a workgroup more: groups of few rows as long as the chip is not full, larger ones then
+    // (us; 32 fp32 rows of 32000 for each of 8 sequences: 1 / 2 / 5 rows a group 16.9 / 16.6 / 21.7; 9 of 128256 for 8: 1 / 3 / 9 rows 18.6 / 15.2 / 24.3,
+    // for 48: 96.2 / 92.2 / 89.1)
     const long long chunks = (vocab + (large ? 16383 : 4095)) / (large ? 16384 : 4096), most = (n * vocab * row_elem(dtype) < 64LL << 20 ? 1024 : 3072) / (large ? 4 : 1);
     long long groups = most / (chunks * n_seqs);
     groups = groups < 1 ? 1 : groups > rows ? rows : groups;

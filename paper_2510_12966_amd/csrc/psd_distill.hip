@@ -10,8 +10,10 @@
 //   distill_row    one workgroup per row, which stays in registers and LDS between the two: read from memory once
 //   distill_tail, distill_grad  (row, chunk): the sums of every chunk; then every chunk joins them, works out the coefficients and
 //                  writes its part of the gradient (the logits read again)
-// Bound: the rows' bytes, read once and written once: 4.9 TB/s (1024 rows of 128256 fp32 entries, 211 us) and 5.3 TB/s (4096 bf16 rows, a quarter of
-// them padding, 347 us) against 4.7 of a large copy; the loss alone reads at 6.7 TB/s.
+// Bound: the rows' bytes, read once and written once: 5.0 TB/s (1024 rows of 128256 fp32 entries, 212 us) and 5.3 TB/s (4096 bf16 rows, a quarter of
+// them padding, 348 us) against 4.7 of a large copy.  The loss alone of 777 bf16 rows of 50257 takes 22.7 us, 3.1 TB/s: an exponential and five
+// more instructions per entry take about as long as the reads, and three workgroups a unit do not hide one behind the other altogether (two groups
+// of vectors on their way, in registers that take turns: 25.2 us).
 // Exponentials and logarithms are fp32, differences, sums and coefficients 64 bits.
 #include "psd_rows.h"
 

@@ -9,7 +9,9 @@
 // radix selection, 8 bits a round.  Items are 64 bits (order-preserving image of the value, complement of the token) and all differ, so that
 // equal values fall in the order of their tokens by themselves.
 // Many rows: one segment each, one launch.  Few rows: several segments, whose lists a second launch merges.
-// Bound: the bytes of the rows, read once.
+// Bound: the bytes of the rows, read once: 6.1 TB/s (64 of 2048 fp32 rows of 128256, 173 us) against 6.6 of a kernel that does nothing else.
+// Few rows: two launches that wait for one another (20 of one such row: 6.1 us for 32 segments, 4.4 for their merge), the larger k is the more
+// the cuts of many candidates (230 of 49 fp32 rows of 65536: 25 us).
 #include "psd_rows.h"
 
 namespace psd {
@@ -478,7 +480,8 @@ __global__ __launch_bounds__(kTopThreads) void top_merge(const TopArgs a) {
 }
 
 // Segments of a row: as many as make the call shortest, counted in blocks that pass one after the other.  1024 workgroups are on the chip at
-// once; a workgroup's start and its last cut take as long as one and a half blocks, the merging launch as long as three.
+// once; a workgroup's start and its last cut take as long as one and a half blocks, the merging launch as long as three (us by segments, fp32 rows
+// of 128256: 1 row 1 / 4 / 16 / 32 segments 37.2 / 21.4 / 13.1 / 10.3; 300 rows 1 / 2 / 3 / 4: 55.8 / 44.1 / 40.7 / 47.3; 900 rows 1 / 2: 83.8 / 90.0).
 static int top_slots(int k) { return k + k / 4 + 32 < kTopThreads ? k + k / 4 + 32 : kTopThreads; }   // what the first threshold lets in, usually
 static int top_segs(int n_rows, int vocab, int k) {
     const int blocks = (vocab + kTopBlock - 1) / kTopBlock;
