@@ -146,6 +146,10 @@ def check_adjusted(got, want, size, dtype):
     (2, 11, 32003, [511, 4100], 300, 5, None, 0),
     (1, 2, 128256, [70000], 0, 2, None, 0),              # a long history: counts of thousands
     (2, 3, 20001, [9000, 14000], 1500, 3, None, 0),      # long histories and long lists of biases
+    (2, 3, 9001, [700, 0], 6000, 2, 9004, 2),            # more biases than a chunk has entries
+    (1, 2, 40003, [20000], 40000, 2, None, 0),           # the same in the largest chunks
+    (24, 12, 20001, [17000] * 23 + [3], 40, 5, None, 0), # several rows of such chunks by one workgroup
+    (300, 1, 32003, [9] * 299 + [5000], 3, 4, None, 0),  # many sequences of one row
 ])
 def test_adjust_matches_oracle(dtype, S, R, V, lengths, n_bias, n_masks, stride, lead):
     rng = np.random.default_rng(V + S)
