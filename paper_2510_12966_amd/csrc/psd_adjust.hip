@@ -333,7 +333,7 @@ extern "C" int psd_adjust_logits(const void* logits, void* out, int32_t dtype, i
         PSD_FAIL(PSD_EINVAL, err, "%s: out overlaps the logits", who);
     AdjustArgs g{logits, out, rows, vocab, rows, 0, 0, logits_stride, out_stride, *adjust};
     psd_adjust& a = g.a;
-    if (a.n_history < 0 || a.n_bias < 0 || a.n_masks < 0 || a.n_masks > 0x7fffffffLL || a.n_bias > 0x7fffffffLL)
+    if (a.n_history < 0 || a.n_bias < 0 || a.n_masks < 0 || a.n_masks > 0x7fffffffLL || a.n_bias > 1LL << 30)
         PSD_FAIL(PSD_EINVAL, err, "%s: n_history=%lld n_bias=%lld n_masks=%lld", who, (long long)a.n_history, (long long)a.n_bias, (long long)a.n_masks);
     if (a.n_history > 0 && (!a.history || !a.history_offsets)) PSD_FAIL(PSD_EINVAL, err, "%s: a history needs its tokens and offsets", who);
     if (a.n_bias > 0 && (!a.bias || !a.bias_tokens || !a.bias_offsets)) PSD_FAIL(PSD_EINVAL, err, "%s: biases need their tokens and offsets", who);

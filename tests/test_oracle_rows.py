@@ -162,6 +162,7 @@ def test_adjust_refusals():
     assert "overlap" in bad(out=_At(0x10000 + 4 * 599))
     bad(adjust=psd.Adjust(history=A, n_history=5)), bad(adjust=psd.Adjust(history_offsets=A, n_history=5)), bad(adjust=psd.Adjust(n_history=-1))
     bad(adjust=psd.Adjust(bias=A, bias_tokens=A, n_bias=5)), bad(adjust=psd.Adjust(bias=A, bias_offsets=A, n_bias=5)), bad(adjust=psd.Adjust(n_bias=-2))
+    bad(adjust=psd.Adjust(bias=A, bias_tokens=A, bias_offsets=A, n_bias=2 ** 30 + 1)), bad(adjust=psd.Adjust(masks=A, mask_index=A, n_masks=2 ** 31))
     bad(adjust=psd.Adjust(masks=A, n_masks=2)), bad(adjust=psd.Adjust(mask_index=A)), bad(adjust=psd.Adjust(n_masks=1, mask_index=A))
     bad(adjust=psd.Adjust(window=A, window_stride=1)), bad(adjust=psd.Adjust(penalties=_At(0x10002)))
     bad(adjust=psd.Adjust(history=A, history_offsets=_At(0x10004), n_history=5))
