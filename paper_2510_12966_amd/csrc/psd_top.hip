@@ -32,10 +32,12 @@ __device__ inline uint32_t rank_of(float z) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ inline float value_of(uint32_t r) { return __uint_as_float(r & 0x80000000u ? r & 0x7fffffffu : ~r); }
-__device__ inline u64 item_of(float z, int v) { return (u64)rank_of(z) << 32 | (uint32_t)~v; }
 
 struct TopLds {
-    alignas(16) u64 list[kTopList];
+    union {
+        alignas(16) u64 list[kTopList];
+        uint2 fresh[kTopList];   // entries that are no items yet: complement of the token, value
+    };
     alignas(16) uint32_t bins[256];
     union {   // (barriers lie between the uses of one and of the other)
         uint32_t hist[3][256];   // one is filled, the next cleared, the last may still be read
@@ -248,7 +250,8 @@ __device__ inline int sort_list(TopLds& l, int n, int k) {
 
 // Frees a list of n <= kTopList items of those whose image is below `least`; how many are left.  All threads, n uniform, after a barrier.
 __device__ inline int thin_list(TopLds& l, int n, uint32_t least) {
-    const int t = threadIdx.x;
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));   // else the caller's loop keeps every place's index in a register
     u64 it[kTopItems];
 #pragma unroll
     for (int i = 0; i < kTopItems; ++i) it[i] = t + kTopThreads * i < n ? l.list[t + kTopThreads * i] : 0;
@@ -295,7 +298,8 @@ __device__ inline int cut_items(TopLds& l, const u64 (&it)[kTopItems], int k) {
 // Cuts a list of n <= kTopList items in the same way.  All threads, n uniform, after a barrier; spoils the bins.
 template <bool NET>
 __device__ inline int cut_list(TopLds& l, int n, int k) {
-    const int t = threadIdx.x;
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));   // as in thin_list
     if (n <= kTopThreads) return sort_list<NET>(l, n, k);
     u64 it[kTopItems];
 #pragma unroll
@@ -353,7 +357,7 @@ __global__ __launch_bounds__(kTopThreads, 4) void top_segment(const TopArgs a) {
     float from = kNoEntry;   // candidates are not below this: the lowest finite value shuts out -inf (and NaN)
     uint32_t least = 0;      // an image that k of the list's items reach, if it has so many (an exact cut leaves it below `from`)
     float base = kNoEntry, scale = 0.f;   // bins: (z - base) scale
-    int n = 0, n_known = 0, done = 0;
+    int n = 0, n_known = 0, n_items = 0, done = 0;   // n_items: those of the list that are items, not yet values and tokens
     // One block, then the load of the one after the next into the same registers: moving a block over would wait for it.  True: the last one.
     auto step = [&](raw16 (&r)[VEC]) {
         const int b = v0 + done * kTopBlock;
@@ -381,37 +385,51 @@ __global__ __launch_bounds__(kTopThreads, 4) void top_segment(const TopArgs a) {
                 scale = bin_scale(l, base);
             }
         }
-        if (__ballot(mx >= from)) {   // a wave takes its places in the list at once; vectors that bring nothing to any lane are passed over
-            bool some[VEC];
+        if (__ballot(mx >= from)) {   // a wave takes its places in the list at once; which lanes bring an entry is a mask per element
+            uint64_t in[VEC * N];
             int brings = 0;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                some[i] = __ballot(vm[i] >= from) != 0;
-                if (some[i]) {
+            for (int i = 0; i < VEC; ++i)
 #pragma unroll
-                    for (int x = 0; x < N; ++x) brings += R::get(r[i], x) >= from;
+                for (int x = 0; x < N; ++x) {
+                    in[i * N + x] = __ballot(R::get(r[i], x) >= from);
+                    brings += __popcll(in[i * N + x]);
+                }
+            int at = 0;
+            if (lane == 0) at = atomicAdd(&l.count, brings);
+            at = __builtin_amdgcn_readfirstlane(at);
+            uint32_t first = ~(uint32_t)(b + N * t);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                asm volatile("" : "+v"(first));   // one vector's tokens at a time are registers enough
+#pragma unroll
+                for (int x = 0; x < N; ++x) {
+                    const uint64_t who = in[i * N + x];
+                    const float z = R::get(r[i], x);
+                    if (z >= from) {
+                        const uint32_t place = __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, at));
+                        l.fresh[place].y = __float_as_uint(z);
+                        __builtin_amdgcn_wave_barrier();   // two stores, or the row's registers would have to be halves of pairs
+                        l.fresh[place].x = first - (uint32_t)(N * kTopThreads * i + x);
+                    }
+                    at += __popcll(who);
                 }
             }
-            const int upto = wave_scan(brings);
-            int at = 0;
-            if (lane == 63) at = atomicAdd(&l.count, upto);
-            at = __builtin_amdgcn_readlane(at, 63) + upto - brings;
-#pragma unroll
-            for (int i = 0; i < VEC; ++i)
-                if (some[i]) {
-#pragma unroll
-                    for (int x = 0; x < N; ++x) {
-                        const float z = R::get(r[i], x);
-                        if (z >= from) {
-                            l.list[at++] = item_of(z, b + N * (t + kTopThreads * i) + x);
-                            if (scale > 0.f) atomicAdd(&l.bins[bin_of(z, base, scale)], 1u);
-                        }
-                    }
-                }
         }
         if (b + 2 * kTopBlock < v1) load(b + 2 * kTopBlock, r);
         __syncthreads();
         n = l.count;
+        if (last || n > kTopLow || (n >= a.k && n >= n_known + 32)) {
+            // the values that came since become items: here a thread has one each, above a whole wave goes through every element of it
+            for (int i = n_items + t; i < n; i += kTopThreads) {
+                const uint2 q = l.fresh[i];
+                const float z = __uint_as_float(q.y);
+                l.list[i] = (u64)rank_of(z) << 32 | q.x;
+                if (scale > 0.f) atomicAdd(&l.bins[bin_of(z, base, scale)], 1u);
+            }
+            n_items = n;
+            __syncthreads();
+        }
         if (scale > 0.f && n >= a.k && (last ? n > kTopThreads : n >= n_known + 32)) {
             const float edge = edge_of(base, scale, kth_bin(l, a.k));
             from = fmaxf(from, edge);
@@ -429,6 +447,7 @@ __global__ __launch_bounds__(kTopThreads, 4) void top_segment(const TopArgs a) {
                     from = value_of(least + 1u);
                 }
             }
+            n_items = n;
         }
         __syncthreads();   // the count has been read by all before the next block adds to it
         return last;
