@@ -105,8 +105,8 @@ __device__ inline uint32_t reached_by(TopLds& l, uint32_t mine, int k) {
     return max(max(quarter, half), max(one, 1u));
 }
 
-// Radix selection among the items it[] of all threads, of which more than k are not 0: the smallest of the k largest.  All threads.
-__device__ inline u64 kth_item(TopLds& l, const u64 (&it)[kTopItems], int k) {
+// Radix selection among the items it[0 .. turns - 1] of all threads, of which more than k are not 0: the smallest of the k largest.  All threads.
+__device__ inline u64 kth_item(TopLds& l, const u64 (&it)[kTopItems], int turns, int k) {
     const int t = threadIdx.x, lane = t & 63;
     l.hist[0][t] = 0;
     __syncthreads();
@@ -117,7 +117,7 @@ __device__ inline u64 kth_item(TopLds& l, const u64 (&it)[kTopItems], int k) {
         const u64 above = shift == 56 ? 0 : ~0ull << (shift + 8);
 #pragma unroll
         for (int i = 0; i < kTopItems; ++i)
-            if (it[i] != 0 && (it[i] & above) == least) atomicAdd(&l.hist[turn][(uint32_t)(it[i] >> shift) & 255], 1u);
+            if (i < turns && it[i] != 0 && (it[i] & above) == least) atomicAdd(&l.hist[turn][(uint32_t)(it[i] >> shift) & 255], 1u);
         __syncthreads();
         // every wave: lane x has bins 255 - 4x .. 252 - 4x; a scan over the lanes finds the bin in which the need-th largest lies
         uint32_t h[4];
@@ -142,21 +142,22 @@ __device__ inline u64 kth_item(TopLds& l, const u64 (&it)[kTopItems], int k) {
     return least;
 }
 
-// Keeps the items of it[] that are not below `least` in the list, in any order; their number.  All threads, after a barrier behind the last
+// Keeps the items of it[0 .. turns - 1] that are not below `least` in the list, in any order; their number.  All threads, after a barrier behind the last
 // use of the list; two barriers.
-__device__ inline int keep_from(TopLds& l, const u64 (&it)[kTopItems], u64 least) {
+__device__ inline int keep_from(TopLds& l, const u64 (&it)[kTopItems], int turns, u64 least) {
     if (threadIdx.x == 0) l.count = 0;
     __syncthreads();
     int keeps = 0;
 #pragma unroll
-    for (int i = 0; i < kTopItems; ++i) keeps += it[i] != 0 && it[i] >= least;
+    for (int i = 0; i < kTopItems; ++i)
+        if (i < turns) keeps += it[i] != 0 && it[i] >= least;
     const int upto = wave_scan(keeps);
     int at = 0;
     if ((threadIdx.x & 63) == 63) at = atomicAdd(&l.count, upto);
     at = __builtin_amdgcn_readlane(at, 63) + upto - keeps;
 #pragma unroll
     for (int i = 0; i < kTopItems; ++i)
-        if (it[i] != 0 && it[i] >= least) l.list[at++] = it[i];
+        if (i < turns && it[i] != 0 && it[i] >= least) l.list[at++] = it[i];
     __syncthreads();
     return l.count;
 }
@@ -248,15 +249,23 @@ __device__ inline int sort_list(TopLds& l, int n, int k) {
     return min(n, k);
 }
 
+// The list's n items into registers, 0 behind them; how many a thread has (the same for all)
+__device__ inline int load_list(const TopLds& l, u64 (&it)[kTopItems], int t, int n) {
+    const int turns = (n + kTopThreads - 1) / kTopThreads;
+#pragma unroll
+    for (int i = 0; i < kTopItems; ++i)
+        if (i < turns) it[i] = t + kTopThreads * i < n ? l.list[t + kTopThreads * i] : 0;
+    return turns;
+}
+
 // Frees a list of n <= kTopList items of those whose image is below `least`; how many are left.  All threads, n uniform, after a barrier.
 __device__ inline int thin_list(TopLds& l, int n, uint32_t least) {
     int t = threadIdx.x;
     asm volatile("" : "+v"(t));   // else the caller's loop keeps every place's index in a register
     u64 it[kTopItems];
-#pragma unroll
-    for (int i = 0; i < kTopItems; ++i) it[i] = t + kTopThreads * i < n ? l.list[t + kTopThreads * i] : 0;
+    const int turns = load_list(l, it, t, n);
     __syncthreads();
-    return keep_from(l, it, (u64)least << 32);
+    return keep_from(l, it, turns, (u64)least << 32);
 }
 
 // The lower edge of bin `bin`, or a few units in the last place less: no entry counted in it may lie below
@@ -270,27 +279,28 @@ __device__ inline float bin_scale(const TopLds& l, float base) {   // after reac
     return width > 1e-30f ? 255.f / width : 0.f;
 }
 
-// Puts the k largest of the items it[] into the list, in descending order; how many there are.  All threads, after a barrier behind the last use of
+// Puts the k largest of the items it[0 .. turns - 1] into the list, in descending order; how many there are.  All threads, after a barrier behind the last use of
 // the list and the bins.
 template <bool NET>
-__device__ inline int cut_items(TopLds& l, const u64 (&it)[kTopItems], int k) {
+__device__ inline int cut_items(TopLds& l, const u64 (&it)[kTopItems], int turns, int k) {
     uint32_t mx = 0;
 #pragma unroll
-    for (int i = 0; i < kTopItems; ++i) mx = max(mx, (uint32_t)(it[i] >> 32));
+    for (int i = 0; i < kTopItems; ++i)
+        if (i < turns) mx = max(mx, (uint32_t)(it[i] >> 32));
     const uint32_t bound = reached_by(l, mx, k);
     l.bins[threadIdx.x] = 0;
-    int n = keep_from(l, it, (u64)bound << 32);
+    int n = keep_from(l, it, turns, (u64)bound << 32);
     const float base = value_of(bound), scale = bound > 1 ? bin_scale(l, base) : 0.f;
     if (n > kTopThreads && scale > 0.f) {
 #pragma unroll
         for (int i = 0; i < kTopItems; ++i)
-            if ((uint32_t)(it[i] >> 32) >= bound) atomicAdd(&l.bins[bin_of(value_of((uint32_t)(it[i] >> 32)), base, scale)], 1u);
+            if (i < turns && (uint32_t)(it[i] >> 32) >= bound) atomicAdd(&l.bins[bin_of(value_of((uint32_t)(it[i] >> 32)), base, scale)], 1u);
         __syncthreads();
-        n = keep_from(l, it, (u64)max(bound, rank_of(edge_of(base, scale, kth_bin(l, k)))) << 32);
+        n = keep_from(l, it, turns, (u64)max(bound, rank_of(edge_of(base, scale, kth_bin(l, k)))) << 32);
     }
     if (n > kTopThreads) {
         __syncthreads();   // the count has been read
-        n = keep_from(l, it, kth_item(l, it, k));
+        n = keep_from(l, it, turns, kth_item(l, it, turns, k));
     }
     return sort_list<NET>(l, n, k);
 }
@@ -302,9 +312,7 @@ __device__ inline int cut_list(TopLds& l, int n, int k) {
     asm volatile("" : "+v"(t));   // as in thin_list
     if (n <= kTopThreads) return sort_list<NET>(l, n, k);
     u64 it[kTopItems];
-#pragma unroll
-    for (int i = 0; i < kTopItems; ++i) it[i] = t + kTopThreads * i < n ? l.list[t + kTopThreads * i] : 0;
-    return cut_items<NET>(l, it, k);
+    return cut_items<NET>(l, it, load_list(l, it, t, n), k);
 }
 
 // The list, sorted, into one row of the outputs
@@ -485,11 +493,12 @@ __global__ __launch_bounds__(kTopThreads) void top_merge(const TopArgs a) {
     const int per = (all + kTopThreads - 1) / kTopThreads;
     u64 it[kTopItems];
 #pragma unroll
-    for (int i = 0; i < kTopItems; ++i) it[i] = i < per && per * t + i < all ? from[per * t + i] : 0;
+    for (int i = 0; i < kTopItems; ++i)
+        if (i < per) it[i] = per * t + i < all ? from[per * t + i] : 0;
     float2 q = make_float2(kNoEntry, 0.f);
     if (a.lse && t < 64)
         for (int i = lane; i < a.segs; i += 64) q = join_sums(q, a.parts[(long long)row * a.segs + i], a.c2);
-    const int n = cut_items<false>(l, it, a.k);
+    const int n = cut_items<false>(l, it, per, a.k);
     put_list(l, n, a.k, a.values + (long long)row * a.k, a.ids + (long long)row * a.k);
     if (a.lse && t < 64) {
         const float m = wave_max_dpp(q.x);
