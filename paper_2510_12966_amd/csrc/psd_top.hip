@@ -2,16 +2,16 @@
 //
 // A workgroup streams over a segment of a row, 4096 entries at a time with the next ones on their way, and keeps a list of candidates in LDS:
 // entries not below a threshold that at least k entries of the segment are known to reach.  The first threshold is one that k of the threads'
-// own maxima in the first block reach.  Entries that enter the list are counted in 256 bins by value, and the lower edge of the bin in which the
-// k-th largest lies is the next threshold; a list that grows too long is freed of what lies below it.  So all but a few hundred entries of a
+// own maxima in the first block reach.  Entries enter the list as they are; once enough have come they are counted in 256 bins by value, and the lower
+// edge of the bin in which the k-th largest lies is the next threshold; a list that grows too long is freed of what lies below it.  So all but a few hundred entries of a
 // row cost a maximum, an exponential and their load.  What is left at the end, or where the bins cannot tell values apart, is cut exactly: ranks
 // come from comparing all pairs of at most 256 items, before that a longer list is filtered by the threads' maxima and, if that leaves too many, by
 // radix selection, 8 bits a round.  Items are 64 bits (order-preserving image of the value, complement of the token) and all differ, so that
 // equal values fall in the order of their tokens by themselves.
 // Many rows: one segment each, one launch.  Few rows: several segments, whose lists a second launch merges.
-// Bound: the bytes of the rows, read once: 6.1 TB/s (64 of 2048 fp32 rows of 128256, 173 us) against 6.6 of a kernel that does nothing else.
+// Bound: the bytes of the rows, read once: 6.1 TB/s (64 of 2048 fp32 rows of 128256, 174 us) against 6.6 of a kernel that does nothing else.
 // Few rows: two launches that wait for one another (20 of one such row: 6.1 us for 32 segments, 4.4 for their merge), the larger k is the more
-// the cuts of many candidates (230 of 49 fp32 rows of 65536: 25 us).
+// the cuts of many candidates (230 of 49 fp32 rows of 65536: 23 us).
 #include "psd_rows.h"
 
 namespace psd {
@@ -222,21 +222,24 @@ __device__ inline void bitonic_sort(TopLds& l, u64& it) {
 
 // Brings the list's n <= 256 items into descending order and drops those behind the k-th; how many are left.  All threads.  A few items by
 // counting the larger ones of each (7 n instructions a wave that has some), more by a bitonic network (about 400) where NET: its straight run pays
-// once many workgroups have brought it into the instruction cache (a launch of one workgroup with 240 items: 8.3 us counting, 15.5 us)
+// once many workgroups have brought it into the instruction cache (a launch of one workgroup with 240 items: 8 us counting, 15.5 us)
 template <bool NET>
 __device__ inline int sort_list(TopLds& l, int n, int k) {
     const int t = threadIdx.x;
     u64 mine = t < n ? l.list[t] : 0;
     int at = t;
     if (!NET || n <= 64) {
-        if (t == n && (n & 1)) l.list[n] = 0;   // pairs
+        if (t >= n && t < ((n + 15) & ~15)) l.list[t] = 0;   // sixteen at a time: their reads need not wait for each other
         __syncthreads();
         if ((t & ~63) < n) {   // waves that have items
             at = 0;
-#pragma unroll 4
-            for (int i = 0; i < n; i += 2) {
-                const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&l.list[i]);
-                at += (o.x > mine) + (o.y > mine);
+#pragma unroll 1
+            for (int i = 0; i < n; i += 16) {
+                ulonglong2 o[8];
+#pragma unroll
+                for (int y = 0; y < 8; ++y) o[y] = *reinterpret_cast<const ulonglong2*>(&l.list[i + 2 * y]);
+#pragma unroll
+                for (int y = 0; y < 8; ++y) at += (o[y].x > mine) + (o[y].y > mine);
             }
         }
     } else if constexpr (NET) {
