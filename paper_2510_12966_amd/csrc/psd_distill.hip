@@ -770,8 +770,9 @@ __global__ __launch_bounds__(kDisThreads) void distill_grad(const DistillArgs a)
 
 // How a call goes: in chunks, or its rows pass by a workgroup of 256, 512 or 1024 threads, or (with a gradient; else they pass by) they are held by
 // one of 256 threads with 32 or 63 vectors each or of 512 with 63.  The loss takes the same sums in the same order with a gradient or without.
-//   chunks   few long rows, which leave most units idle otherwise (us, chunks / passing; 65536 fp32 entries: 48 rows 11.6 / 13.3, 96 rows
-//            15.1 / 13.9; 128256: 16 rows 12.6 / 20.9, 48 rows 22.7 / 21.6; bf16: 48 rows 14.2 / 18.9, 96 rows 20.9 / 19.6), and rows over 1 MB
+//   chunks   few long rows, which leave most units idle otherwise: 12 MB of them, 20 MB where a row has 256 KB (us, chunks / passing; 65536 fp32
+//            entries: 64 rows 12.9 / 13.8, 89 rows 14.9 / 14.1; 128256: 29 rows 17.2 / 21.7, 48 rows 22.9 / 22.0; bf16: 64 rows 16.3 / 19.5, 89 rows
+//            21.3 / 19.7; 65536 bf16: 64 rows 12.0 / 12.7, 108 rows 15.3 / 13.2), and rows over 1 MB
 //   holding  rows from 96 KB, 240 MB of them in all: there the second pass comes from memory (passing / holding; 128256 fp32 entries: 800 rows
 //            195 / 178, 300 rows 76 / 73; bf16: 2000 rows 238 / 205, 800 rows 97 / 100; 50257 bf16: 3000 rows 196 / 170, 1200 rows 72 / 79)
 //   passing  1024 threads for at most a row per unit, 512 for rows over 128 KB (65536 fp32 entries, 2000 rows: 237, with 256 threads 291), else 256
@@ -779,7 +780,7 @@ __global__ __launch_bounds__(kDisThreads) void distill_grad(const DistillArgs a)
 enum Way { PASS_256, PASS_512, PASS_1024, HOLD_128K, HOLD_252K, HOLD_504K, CHUNKS };
 static Way way_of(int n_rows, int vocab, int el, int k) {
     const long long vectors = ((long long)vocab * el + 15) / 16, all = vectors * 16 * n_rows;
-    if (vectors > 1024 * 64 || (vocab >= 49152 && all <= 14LL << 20)) return CHUNKS;
+    if (vectors > 1024 * 64 || (vocab >= 49152 && all <= (vectors >= 16384 ? 20LL : 12LL) << 20)) return CHUNKS;
     if (n_rows <= 256 || vectors > 512 * 64) return PASS_1024;
     const bool narrow = k < kPlaces;   // thread k must have no place
     if (vectors >= 6144 && vectors <= 512 * 63 && all >= 240LL << 20) return narrow && vectors <= 256 * 32 ? HOLD_128K : narrow && vectors <= 256 * 63 ? HOLD_252K : HOLD_504K;
