@@ -359,7 +359,7 @@ extern "C" int psd_adjust_logits(const void* logits, void* out, int32_t dtype, i
     // Every group of rows reads the lists again and leaves a workgroup more: groups of few rows as long as the chip is not full, larger ones then
     // (us; 32 fp32 rows of 32000 for each of 8 sequences: 1 / 2 / 5 rows a group 16.9 / 16.6 / 21.7; 9 of 128256 for 8: 1 / 3 / 9 rows 18.6 / 15.2 / 24.3,
     // for 48: 96.2 / 92.2 / 89.1)
-    const long long chunks = (vocab + (large ? 16383 : 4095)) / (large ? 16384 : 4096), most = (n * vocab * row_elem(dtype) < 64LL << 20 ? 1024 : 3072) / (large ? 4 : 1);
+    const long long chunks = (vocab + (large ? 16383 : 4095)) / (large ? 16384 : 4096), most = (n * vocab * row_elem(dtype) < 64LL << 20 ? 1024 : 3 * 1024) / (large ? 4 : 1);
     long long groups = most / (chunks * n_seqs);
     groups = groups < 1 ? 1 : groups > rows ? rows : groups;
     g.group = (int)((rows + groups - 1) / groups);
