@@ -382,8 +382,9 @@ int psd_top_logits(const void* logits, int32_t dtype, int32_t n_rows, int32_t vo
  *   p_i = exp(value_i / temperature - lse) with the record's lse (taken at the same temperature); without (top_lse NULL) the record
  *   is the whole teacher: p = softmax of its values / temperature
  *   Outcomes: the tokens of S, and one more for all others together: p_rest = max(0, 1 - sum p_i), or 0 where the record is
- *   complete or S the whole vocabulary; q_rest = the student's mass outside S.  Where the student has no entry outside S, a p_rest up to
- *   (2 + |lse|) 2^-22 is taken for the rounding of a record that holds all of the teacher's entries, and counts as 0.
+ *   complete or S the whole vocabulary; q_rest = the student's mass outside S.  Where the student has no mass outside S (its entries there are
+ *   -inf, or each below 2^-126 of its largest entry's), a p_rest up to (2 + |lse|) 2^-22 is taken for the rounding of a record that
+ *   holds all of the teacher's entries, and counts as 0.
  *   PSD_DIV_KL   sum p ln(p / q)          PSD_DIV_JSD   Div of this library on these outcomes: never above Div of the whole rows
  *   loss[r] = row_weights[r] * divergence,  grad[r][v] = d loss[r] / d z[r][v]
  * row_weights NULL: 1 everywhere.  A row of weight 0 (padding), or without a valid place, has loss 0 and gradient 0; its student row

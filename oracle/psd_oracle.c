@@ -248,6 +248,8 @@ void orc_distill_row(const float* z, int V, const float* values, const int32_t* 
     double top, rest_top, l = 0.0, sum_w = 0.0;
     const double all = log_sum(z, V, T, NULL, &top), rest = log_sum(z, V, T, in_s, &rest_top);
     const double l_rest = rest_top > -INFINITY ? rest_top - top + rest - all : -INFINITY;
+    /* a remainder that roundings of the fp32 lse may have left, where the student has no mass beside the record */
+    if (lse && p[n] <= (2.0 + fabs((double)*lse)) * 0x1p-22 && (rest_top - top) * 1.4426950408889634 < -126.0) p[n] = 0.0;
     for (int i = 0; i <= n; ++i) {
         const double lq = i < n ? z[tok[i]] / T - top - all : l_rest, q = exp(lq);
         if (divergence == 0) {

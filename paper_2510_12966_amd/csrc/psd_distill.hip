@@ -220,9 +220,10 @@ __device__ inline RowSums row_sums(const DistillArgs& a, const PlaceLds& l, floa
     r.p_place = a.lse ? 1.0 : 1.0 / s;
     r.mass = a.lse ? s : 1.0;
     // A negative token: the teacher has no entries beside those of its record.  A record that just holds them all has none, and then 1 - s is
-    // what the roundings leave (lse is a float, off by 2^-24 of itself, its logarithm and the p by a few 2^-24 more): a student that has no
-    // entry beside them either is not held to it, for that would cost it an infinite divergence.
-    const bool noise = tail.y == 0.f && 1.0 - s <= (2.0 + fabs((double)l.lse)) * 0x1p-22;
+    // what the roundings leave (lse is a float, off by 2^-24 of itself, its logarithm and the p by a few 2^-24 more): a student without mass
+    // beside them is not held to it, for whether a mask closes its entries by -inf or by a large negative number, that would cost it a remainder
+    // of nothing times the logarithm of nothing.
+    const bool noise = (tail.y == 0.f || r.tail_shift < -126.f) && 1.0 - s <= (2.0 + fabs((double)l.lse)) * 0x1p-22;
     r.p_rest = a.lse && sum_of(l.open) == 0 && sum_of(l.valid) < a.V && s < 1.0 && !noise ? 1.0 - s : 0.0;
     r.scale = (double)weight * a.inv_temp;
     return r;

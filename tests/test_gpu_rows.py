@@ -606,6 +606,32 @@ def test_distill_a_record_that_just_holds_a_grammars_tokens():
         assert np.isposinf(loss).all()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("closed", [-1e9, -3.3895313892515355e38, -INF])
+def test_distill_grammar_records_under_masks_of_any_low_value(dtype, closed):
+    """A mask may be a large negative number as well as -inf: what roundings leave of a record that holds all of its row is not held against a
+    student that has no mass beside it either.  The bounds are those of the test above, h of a gradient stored as bf16 more."""
+    rng = np.random.default_rng(37)
+    for n, V, allow, k in ((64, 1000, 2, 2), (64, 5000, 7, 7), (64, 5000, 7, 10), (300, 5000, 64, 64), (20, 128256, 3, 3)):
+        t, z = pair(rng, n, V, dtype, spread=8)
+        allowed = np.argpartition(rng.random((n, V)), allow, axis=1)[:, :allow]
+        shut = np.ones((n, V), bool)
+        np.put_along_axis(shut, allowed, False, axis=1)
+        t[shut], z[shut] = closed, rounded(closed, dtype)
+        values, ids, lse = run_top(Rows(t, psd.F32), n, V, k, 1.0, psd.F32)
+        a, b = (np.take_along_axis(y, allowed, 1).astype(np.float64) for y in (t, z))
+        lp, lq = a - np.logaddexp.reduce(a, 1, keepdims=True), b - np.logaddexp.reduce(b, 1, keepdims=True)
+        p, q = np.exp(lp), np.exp(lq)
+        mid = np.log((p + q) / 2)
+        kl_p, kl_q = p * (lp - mid), q * (lq - mid)
+        tol = 2.0 ** -20 * (2 + np.abs(lse)) * (1 + np.abs(lp - lq).max(1))
+        for div, want, wg in ((psd.DIV_KL, (p * (lp - lq)).sum(1), q - p), (psd.DIV_JSD, (kl_p + kl_q).sum(1) / 2, (kl_q - q * kl_q.sum(1, keepdims=True)) / 2)):
+            loss, grad = run_distill(Rows(z, dtype), n, V, values, ids, lse, k, 1.0, div, None, dtype)
+            assert (np.abs(loss - want) <= tol).all(), (V, div, np.abs(loss - want).max())
+            assert (grad[shut] == 0).all()
+            assert (np.abs(np.take_along_axis(grad, allowed, 1) - wg) <= tol[:, None] + (H * (np.abs(wg) + tol[:, None]) if dtype == psd.BF16 else 0)).all()
+
+
 def test_distill_gradient_is_that_of_differences_of_its_own_loss():
     rng = np.random.default_rng(8)
     V, k, T = 300, 9, 1.0

@@ -127,6 +127,31 @@ def test_distill_row_edges():
     assert abs(loss) < 1e-12 and np.abs(grad).max() < 1e-7
 
 
+@pytest.mark.parametrize("closed", [-INF, -1e9, -3.402823466e38])
+def test_a_record_that_just_holds_a_grammars_tokens(closed):
+    """Its fp32 lse leaves a remainder of up to some 2^-24: the student, closed in the same places, is not held to it."""
+    rng = np.random.default_rng(7)
+    left = 0
+    for _ in range(100):
+        V, k = 200, 8
+        allowed = rng.choice(V, k, replace=False)
+        t, z = np.full((2, V), closed, np.float32)
+        t[allowed], z[allowed] = rng.normal(0, 4, (2, k))
+        values, ids, lse = oracle.top_row(t, k)
+        p, q = scipy.special.softmax(t[allowed].astype(np.float64)), scipy.special.softmax(z[allowed].astype(np.float64))
+        left += np.exp(values - float(np.float32(lse))).sum() < 1
+        # every ln p is off by 2^-24 |lse|, and that much of the mass is left out
+        tol = 2.0 ** -23 * (1 + abs(lse)) * (1 + np.abs(np.log(p / q)).max())
+        loss, grad = oracle.distill_row(z, values, ids, lse)
+        assert abs(loss - scipy.special.rel_entr(p, q).sum()) <= tol and np.abs(grad[allowed] - (q - p)).max() <= tol
+        assert (np.delete(grad, allowed) == 0).all()
+        assert abs(oracle.distill_row(z, values, ids, lse, divergence=1)[0] - scipy.spatial.distance.jensenshannon(p, q) ** 2) <= tol
+    assert 20 < left < 80
+    # a true remainder counts: the student has e^closed for it
+    loss, _ = oracle.distill_row(z, values, ids, lse + 0.01)
+    assert loss > 1e6 if np.isfinite(closed) else loss == INF
+
+
 # ---- refusals (argument checks come before anything touches a GPU) ----------------------------------------
 
 class _At:
