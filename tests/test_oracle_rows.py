@@ -247,6 +247,31 @@ def test_host_arrays_are_refused():
         psd.distill(A, 1, 100, A, A, A, 4, 1.0, psd.DIV_KL, None, A, host, A, 1 << 20)
 
 
+class _OnHost(_At):
+    """What a tensor in host memory looks like: it has an address, but not one for a kernel."""
+    is_cuda = False
+
+
+def test_tensors_in_host_memory_are_refused():
+    torch = pytest.importorskip("torch")
+    ws = 1 << 20
+    for host in (_OnHost(), torch.zeros(100), torch.zeros(100, device="meta")):
+        for name in ("history", "history_offsets", "n_prompt", "window", "penalties", "bias_tokens", "bias", "bias_offsets", "masks", "mask_index"):
+            with pytest.raises(TypeError):
+                psd.Adjust(**{name: host})
+        calls = [(psd.adjust_logits, dict(logits=A, out=B, n_seqs=1, rows=1, vocab=100, adjust=psd.Adjust()), ("logits", "out")),
+                 (psd.top_logits, dict(logits=A, n_rows=1, vocab=100, k=4, temperature=1.0, values=B, ids=B, lse=B, workspace=B, workspace_bytes=ws),
+                  ("logits", "values", "ids", "lse", "workspace")),
+                 (psd.distill, dict(logits=A, n_rows=1, vocab=100, top_values=B, top_ids=B, top_lse=B, k=4, temperature=1.0, divergence=psd.DIV_KL, row_weights=B,
+                                    loss=B, grad=None, workspace=B, workspace_bytes=ws),
+                  ("logits", "top_values", "top_ids", "top_lse", "row_weights", "loss", "grad", "workspace"))]
+        for fn, ok, names in calls:
+            for name in names:
+                # (a dtype that does not exist: were the buffer taken, the call would still be refused, by another error)
+                with pytest.raises(TypeError):
+                    fn(**{**ok, name: host, "dtype": 9})
+
+
 def test_adjust_struct_has_the_layout_of_the_header():
     import ctypes
     A = psd.Adjust
