@@ -380,7 +380,8 @@ int psd_top_logits(const void* logits, int32_t dtype, int32_t n_rows, int32_t vo
  *   outside 0 .. vocab - 1, or stands in an earlier place of the row already, is passed over; a negative token also says that the
  *   record is complete: the teacher has no entries beside it (a row under a grammar's mask, say)
  *   p_i = exp(value_i / temperature - lse) with the record's lse (taken at the same temperature); without (top_lse NULL) the record
- *   is the whole teacher: p = softmax of its values / temperature
+ *   is the whole teacher: p = softmax of its values / temperature.  Such an exponential (without lse: that of the difference from the
+ *   largest value) below 2^-126 counts as 0, and an outcome of p = 0 costs KL nothing, whatever the student has there
  *   Outcomes: the tokens of S, and one more for all others together: p_rest = max(0, 1 - sum p_i), or 0 where the record is
  *   complete or S the whole vocabulary; q_rest = the student's mass outside S.  Where the student has no mass outside S (its entries there are
  *   -inf, or each below 2^-126 of its largest entry's), a p_rest up to (2 + |lse|) 2^-22 is taken for the rounding of a record that

@@ -241,7 +241,11 @@ void orc_distill_row(const float* z, int V, const float* values, const int32_t* 
         free(in_s); free(tok); free(p); free(w);
         return;
     }
-    for (int i = 0; i < n; ++i) total += p[i] = exp(p[i] - (lse ? (double)*lse : m));
+    for (int i = 0; i < n; ++i) {
+        p[i] = exp(p[i] - (lse ? (double)*lse : m));
+        if (p[i] < 0x1p-126) p[i] = 0.0;
+        total += p[i];
+    }
     p[n] = 0.0;
     if (lse) p[n] = complete || n == V || total >= 1.0 ? 0.0 : 1.0 - total;
     else for (int i = 0; i < n; ++i) p[i] /= total;

@@ -85,11 +85,11 @@ __device__ inline float max_of(const float (&s)[kPlaceWaves]) { return fmaxf(fma
 __device__ inline int sum_of(const int (&s)[kPlaceWaves]) { return (s[0] + s[1]) + (s[2] + s[3]); }
 __device__ inline double x_times(double x, double y) { return x > 0.0 ? x * y : 0.0; }   // 0 ln 0 = 0
 
-// e^x of a 64-bit x on the hardware's exponential: the argument as a rounded float and the rest
+// e^x of a 64-bit x on the hardware's exponential: the argument as a rounded float and the rest.  0 where it is below 2^-126.
 __device__ inline float exp_of(double x) {
-    const double y = fmax(x * 1.4426950408889634, -200.0);
+    const double y = x * 1.4426950408889634;
     const float hi = (float)y;
-    return fast_exp2(hi) * fmaf((float)(y - (double)hi), kLn2, 1.f);
+    return y >= -126.0 ? fast_exp2(hi) * fmaf((float)(y - (double)hi), kLn2, 1.f) : 0.f;
 }
 
 // ln(2 x / (x + y)).  Near x = y by the odd series of 2 artanh(u) = ln((1 + u) / (1 - u)), u = (x - y) / (3 x + y), which loses nothing there
@@ -270,7 +270,7 @@ __device__ inline float row_loss(const DistillArgs& a, const PlaceLds& l, float 
     if (a.divergence == PSD_DIV_KL) {
         const double log_total = log(r.total), lq_rest = (double)r.tail_shift * kLn2d + (double)logf(tail.y) - log_total;
         const double d = sum_of(l.sums[2]) * r.p_place + (a.lse ? 0.0 : log(r.p_place));
-        loss = d - r.mass * ((double)r.z_shift * kLn2d - log_total) + x_times(r.p_rest, (double)logf((float)r.p_rest) - lq_rest);
+        loss = d - x_times(r.mass, (double)r.z_shift * kLn2d - log_total) + x_times(r.p_rest, (double)logf((float)r.p_rest) - lq_rest);
     } else {
         const float pr = (float)r.p_rest, qr = (float)r.q_rest;
         loss = 0.5 * (sum_of(l.sums[3]) + x_times(pr, log_share(pr, qr)) + x_times(qr, log_share(qr, pr)));

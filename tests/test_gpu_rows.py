@@ -632,6 +632,27 @@ def test_distill_grammar_records_under_masks_of_any_low_value(dtype, closed):
             assert (np.abs(np.take_along_axis(grad, allowed, 1) - wg) <= tol[:, None] + (H * (np.abs(wg) + tol[:, None]) if dtype == psd.BF16 else 0)).all()
 
 
+@pytest.mark.parametrize("n,V", [(5, 3), (5, 5000), (20, 128256)])
+def test_distill_a_record_without_probability(n, V):
+    """Places whose p fp32 does not hold are outcomes of probability 0, whatever the student has there."""
+    rng = np.random.default_rng(V)
+    k, low = 2, -3.402823466e38
+    z = rng.normal(0, 2, (5, V)).astype(np.float32)
+    ids = np.array([[1, V], [1, V], [0, 1], [1, -1], [1, 0]], np.int32)
+    values = np.array([[-INF, 5], [-200, 5], [-88, -300], [-200, -INF], [-200, -120]], np.float32)
+    for r in range(5):
+        z[r, [v for v in ids[r] if 0 <= v < V]] = -INF if r < 4 else low
+    lse = np.zeros(5, np.float32)
+    at = np.arange(n) % 5
+    for T in (1.0, 0.5):
+        loss, grad = run_distill(Rows(z[at], psd.F32), n, V, values[at], ids[at], lse[at], k, T, psd.DIV_KL, None, psd.F32)
+        # 1 ln(1 / q_rest) with q_rest = 1: a logarithm of at most ln V in fp32 (off by 2 u of itself) less the same in 64 bits; the complete record has nothing
+        assert (np.abs(loss) <= 4 * U * (1 + np.log(V))).all(), loss
+        assert (np.abs(grad) <= 2 * U / T).all()
+        loss, grad = run_distill(Rows(z[at], psd.F32), n, V, values[at], ids[at], lse[at], k, T, psd.DIV_JSD, None, psd.F32)
+        assert (np.abs(loss - np.where(at == 3, np.log(2) / 2, 0)) <= 8 * U).all() and (np.abs(grad) <= 8 * U / T).all()
+
+
 def test_distill_gradient_is_that_of_differences_of_its_own_loss():
     rng = np.random.default_rng(8)
     V, k, T = 300, 9, 1.0

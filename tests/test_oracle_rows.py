@@ -152,6 +152,22 @@ def test_a_record_that_just_holds_a_grammars_tokens(closed):
     assert loss > 1e6 if np.isfinite(closed) else loss == INF
 
 
+@pytest.mark.parametrize("low", [-INF, -1e9, -3.402823466e38])
+def test_outcomes_of_no_probability_cost_nothing(low):
+    """A teacher's place whose exponential fp32 does not hold, at a token that the student has closed."""
+    z = np.array([1.0, low, 0.5, low], np.float32)
+    lq = np.log(np.exp([1.0, 0.5]).sum())
+    for v in (-INF, -200.0, -88.0):
+        loss, grad = oracle.distill_row(z, [v, v], [1, 3], 0.0)              # all of the teacher lies beside its record
+        assert abs(loss) < 1e-15 and np.abs(grad).max() < 1e-15
+        loss, grad = oracle.distill_row(z, [1.0, v], [0, 1], np.float32(1.0))   # one sure token: p = 1
+        assert abs(loss - (lq - 1.0)) < 1e-12 and grad[1] == 0
+        loss, grad = oracle.distill_row(z, [2.0, v], [0, 1], None)
+        assert abs(loss - (lq - 1.0)) < 1e-12 and grad[1] == 0
+    if low == -INF:
+        assert oracle.distill_row(z, [1.0, -80.0], [0, 1], np.float32(1.0))[0] == INF      # e^-81 is held
+
+
 # ---- refusals (argument checks come before anything touches a GPU) ----------------------------------------
 
 class _At:
