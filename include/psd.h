@@ -390,7 +390,7 @@ int psd_top_logits(const void* logits, int32_t dtype, int32_t n_rows, int32_t vo
  *   loss[r] = row_weights[r] * divergence,  grad[r][v] = d loss[r] / d z[r][v]
  * row_weights NULL: 1 everywhere.  A row of weight 0 (padding), or without a valid place, has loss 0 and gradient 0; its student row
  * is not looked at.  KL is +inf where the student has no mass that fp32 holds for an outcome of the teacher; a student row without any entry
- * above -inf has loss NaN.  row_weights is also where a gradient with respect to the losses goes: a second call then yields the product.
+ * above -inf, or a record without top_lse that has places but no value above -inf, has loss and gradient NaN.  row_weights is also where a gradient with respect to the losses goes: a second call then yields the product.
  *   top_values, top_ids [n_rows][k], 1 <= k <= PSD_MAX_TOP; top_lse, row_weights, loss [n_rows]
  *   grad: rows as the logits', of their type, grad_stride apart; NULL: the loss alone.  It may be `logits` itself (with equal
  *   strides); other overlaps are refused.

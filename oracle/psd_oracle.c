@@ -267,8 +267,11 @@ void orc_distill_row(const float* z, int V, const float* values, const int32_t* 
         }
         sum_w += w[i];
     }
-    *loss = all == -INFINITY ? NAN : weight * l;
-    if (grad) {
+    const int none = all == -INFINITY || (!lse && !(total > 0.0));    /* no distribution on one of the sides */
+    *loss = none ? NAN : weight * l;
+    if (grad && none) {
+        for (int v = 0; v < V; ++v) grad[v] = NAN;
+    } else if (grad) {
         /* within the others the derivative spreads by their own distribution */
         for (int v = 0; v < V; ++v)
             if (!in_s[v]) {

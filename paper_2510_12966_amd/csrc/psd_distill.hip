@@ -204,6 +204,7 @@ __device__ inline void place_second(const DistillArgs& a, PlaceLds& l, uint32_t 
 struct RowSums {
     double total, q_place, q_rest, p_place, mass, p_rest;   // mass: sum of the places' p
     double scale;
+    bool none;           // the student's row or the record is no distribution at all
     float z_shift;       // (z_max - m) c2 and (tail's maximum - m) c2 in base 2, m the larger of the two
     float tail_shift;
 };
@@ -226,6 +227,7 @@ __device__ inline RowSums row_sums(const DistillArgs& a, const PlaceLds& l, floa
     const bool noise = (tail.y == 0.f || r.tail_shift < -126.f) && 1.0 - s <= (2.0 + fabs((double)l.lse)) * 0x1p-22;
     r.p_rest = a.lse && sum_of(l.open) == 0 && sum_of(l.valid) < a.V && s < 1.0 && !noise ? 1.0 - s : 0.0;
     r.scale = (double)weight * a.inv_temp;
+    r.none = !(r.total > 0.0) || !(a.lse || s > 0.0);
     return r;
 }
 
@@ -253,13 +255,12 @@ __device__ inline float place_gradient(const DistillArgs& a, PlaceLds& l, const 
         g_rest = 0.5 * fma(-r.q_rest, W, kqr);
         g = 0.5 * fma(-q, W, x_times((float)q, log_share((float)q, (float)p)));
     }
-    const bool none = !(r.total > 0.0);   // no distribution at all
     if (t == 0) {
-        l.rest = none ? NAN : tail.y > 0.f ? (float)(g_rest * r.scale / tail.y) : 0.f;
+        l.rest = r.none ? NAN : tail.y > 0.f ? (float)(g_rest * r.scale / tail.y) : 0.f;
         l.rest_max = tail.x;
         l.tail = tail;
     }
-    return none ? NAN : (float)(g * r.scale);
+    return r.none ? NAN : (float)(g * r.scale);
 }
 
 // one thread, after place_gradient
@@ -275,7 +276,7 @@ __device__ inline float row_loss(const DistillArgs& a, const PlaceLds& l, float 
         const float pr = (float)r.p_rest, qr = (float)r.q_rest;
         loss = 0.5 * (sum_of(l.sums[3]) + x_times(pr, log_share(pr, qr)) + x_times(qr, log_share(qr, pr)));
     }
-    return r.total > 0.0 ? (float)(loss * weight) : NAN;
+    return r.none ? NAN : (float)(loss * weight);
 }
 
 // joins one (maximum, sum) per lane over the wave

@@ -653,6 +653,23 @@ def test_distill_a_record_without_probability(n, V):
         assert (np.abs(loss - np.where(at == 3, np.log(2) / 2, 0)) <= 8 * U).all() and (np.abs(grad) <= 8 * U / T).all()
 
 
+@pytest.mark.parametrize("n,V", [(3, 5000), (20, 128256)])
+@pytest.mark.parametrize("div", [psd.DIV_KL, psd.DIV_JSD])
+def test_distill_a_whole_record_without_an_entry_is_no_distribution(n, V, div):
+    rng = np.random.default_rng(V)
+    z = rng.normal(0, 2, (n, V)).astype(np.float32)
+    values = np.tile(np.array([-INF, -INF, -INF], np.float32), (n, 1))
+    ids = np.tile(np.array([4, 9, 7], np.int32), (n, 1))
+    values[1, 1] = 0.5                              # one entry is a distribution
+    ids[2] = -1                                     # no place at all is padding
+    loss, grad = run_distill(Rows(z, psd.F32), n, V, values, ids, None, 3, 1.0, div, None, psd.F32)
+    assert np.isnan(loss[0]) and np.isnan(grad[0]).all()
+    assert loss[2] == 0 and (grad[2] == 0).all()
+    check_distill(z[1:2], values[1:2], ids[1:2], None, 1.0, div, None, loss[1:2], grad[1:2], psd.F32)
+    only, _ = run_distill(Rows(z, psd.F32), n, V, values, ids, None, 3, 1.0, div, None, psd.F32, want_grad=False)
+    assert only.tobytes() == loss.tobytes()
+
+
 def test_distill_gradient_is_that_of_differences_of_its_own_loss():
     rng = np.random.default_rng(8)
     V, k, T = 300, 9, 1.0

@@ -168,6 +168,18 @@ def test_outcomes_of_no_probability_cost_nothing(low):
         assert oracle.distill_row(z, [1.0, -80.0], [0, 1], np.float32(1.0))[0] == INF      # e^-81 is held
 
 
+@pytest.mark.parametrize("div", [0, 1])
+def test_a_side_without_an_entry_is_no_distribution(div):
+    z = np.array([1.0, 0.0, -1.0, 0.5], np.float32)
+    for args in ((z, [-INF, -INF], [0, 3], None), (np.full(4, -INF, np.float32), [2.0, 1.0], [0, 3], 3.0)):
+        loss, grad = oracle.distill_row(*args, divergence=div)
+        assert np.isnan(loss) and np.isnan(grad).all()
+    loss, grad = oracle.distill_row(z, [-INF, -3.402823466e38], [0, 3], None, divergence=div)     # the lowest value is an entry
+    assert np.isfinite(loss) and abs(grad.sum()) < 1e-12
+    loss, grad = oracle.distill_row(z, [-INF, -INF], [0, 3], 3.0, divergence=div)                 # with the row's lse all of it lies outside
+    assert np.isfinite(loss) and abs(grad.sum()) < 1e-12
+
+
 # ---- refusals (argument checks come before anything touches a GPU) ----------------------------------------
 
 class _At:
