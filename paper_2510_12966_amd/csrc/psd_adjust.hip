@@ -35,12 +35,13 @@ __device__ inline void clamp_list(int64_t& lo, int64_t& hi, int64_t n) {
 
 typedef int32_t four_tokens __attribute__((ext_vector_type(4), aligned(4)));
 
-struct Penalty { float repetition, inverse, presence, frequency; };   // inverse: 1 / repetition
+struct Penalty { float repetition, divisor, up, inverse, presence, frequency; };   // divisor: repetition * up, inverse: 1 / divisor
 
 // One logit.  The quotient comes from the rounded inverse and one correction by its remainder (exact in the fused multiply-add); one beyond
-// the largest float has no remainder and stays infinite.
+// the largest float has no remainder and stays infinite.  A repetition so small that its inverse is no float is taken 2^64 times as large, and the
+// logit with it (where that passes the largest float, the quotient does as well).
 __device__ inline float adjusted(float z, uint32_t count, const Penalty& p) {
-    const float q = z * p.inverse, corrected = fmaf(fmaf(-q, p.repetition, z), p.inverse, q), quotient = corrected == corrected ? corrected : q;
+    const float n = z * p.up, q = n * p.inverse, corrected = fmaf(fmaf(-q, p.divisor, n), p.inverse, q), quotient = corrected == corrected ? corrected : q;
     const float y = z > 0.f ? quotient : z * p.repetition;
     const uint32_t occurrences = count & ~kPromptOnly;
     const float minus = occurrences ? fmaf((float)occurrences, p.frequency, p.presence) : 0.f;
@@ -291,7 +292,7 @@ __global__ __launch_bounds__(NT, 4) void adjust_rows(const AdjustArgs g) {
     const auto* pens = (const __attribute__((address_space(4))) float*)(a.penalties ? (uint64_t)(a.penalties + 3 * (int64_t)s) : here);
     const int more = a.mask_index ? j1 - 1 - j0 : 0;
     Lists lists{off[0], off[1], prompt[0], boff[0], boff[1], mask[0], mask[min(1, more)], mask[min(2, more)]};
-    Penalty pen{pens[0], 0.f, pens[1], pens[2]};
+    Penalty pen{pens[0], 1.f, 1.f, 1.f, pens[1], pens[2]};
     if (g.counts | g.biases)
         for (int i = threadIdx.x; i < (CHUNK + 64 + CHUNK / 32 + 4) / 4; i += NT) lds[i] = make_uint4(0, 0, 0, 0);
     clamp_list(lists.lo, lists.hi, a.n_history);
@@ -300,9 +301,11 @@ __global__ __launch_bounds__(NT, 4) void adjust_rows(const AdjustArgs g) {
     if (!a.history) lists.hi = lists.lo;
     if (!a.bias) lists.b1 = lists.b0;
     if (!a.mask_index) lists.m0 = lists.m1 = lists.m2 = -1;
-    if (!a.penalties) pen = Penalty{1.f, 1.f, 0.f, 0.f};
+    if (!a.penalties) pen = Penalty{1.f, 1.f, 1.f, 1.f, 0.f, 0.f};
     if (!(pen.repetition > 0.f)) pen.repetition = 1.f;
-    pen.inverse = 1.f / pen.repetition;
+    pen.up = pen.repetition < 0x1p-120f ? 0x1p64f : 1.f;
+    pen.divisor = pen.repetition * pen.up;
+    pen.inverse = 1.f / pen.divisor;
     if (v0 + CHUNK <= g.V) adjust_group<BF16, NT, PARTS, true>(g, lists, l, pen, s, v0, j0, j1);
     else adjust_group<BF16, NT, PARTS, false>(g, lists, l, pen, s, v0, j0, j1);
 }

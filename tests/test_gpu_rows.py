@@ -235,6 +235,28 @@ def test_adjust_penalties_far_from_one(dtype):
     assert (err <= np.abs(want[inside]) * ((H if dtype == psd.BF16 else 0) + 2 * U) + 2e-38).all()   # two roundings, and what lies below the smallest normal
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_adjust_the_smallest_repetitions(dtype):
+    """Quotients by numbers whose inverse no float holds, with the bounds of the test above."""
+    reps = np.array([1.17549435e-38, 5e-39, 2.9e-39, 1e-40, 1.4e-45, 2.0 ** -100, 1e-31], np.float32)
+    z = np.tile(np.array([1e-3, 0.25, 1e-7, 5, 0, -0.0, -5, 1e-20, -INF, 3e38, -3e38, 1e-37, 0.9], np.float32), (reps.size, 1))
+    z = rounded(z, dtype)
+    S, V = z.shape
+    x, y = Rows(z, dtype), Rows(np.zeros((S, V)), dtype)
+    history = np.tile(np.arange(V, dtype=np.int32), S)
+    pen = np.stack((reps, 0 * reps, 0 * reps), 1)
+    psd.adjust_logits(x, y, S, 1, V, psd.Adjust(history=dev(history), history_offsets=dev(np.arange(S + 1, dtype=np.int64) * V), n_history=history.size, penalties=dev(pen)), dtype=dtype)
+    psd.dev_sync()
+    r = reps[:, None].astype(np.float64)
+    want = np.where(z > 0, z / r, z * r)
+    big = float(np.finfo(np.float32).max) if dtype == psd.F32 else 3.3895313892515355e38
+    got = y.get()
+    inside = np.abs(want) <= big
+    assert np.array_equal(got[~inside], np.sign(want[~inside]) * INF)
+    err = np.abs(got[inside] - want[inside])
+    assert (err <= np.abs(want[inside]) * ((H if dtype == psd.BF16 else 0) + 2 * U) + 2e-38).all()
+
+
 def test_rows_far_apart():
     """Rows more than 2^31 elements apart: every offset is taken in 64 bits."""
     rng = np.random.default_rng(9)
