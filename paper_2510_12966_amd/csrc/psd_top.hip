@@ -327,13 +327,14 @@ __device__ inline void put_list(const TopLds& l, int n, int k, float* values, in
     ids[t] = t < n ? (int32_t)~(uint32_t)it : -1;
 }
 
-__device__ inline float lse_of(float2 p, float inv_temp) { return p.y > 0.f ? (float)((double)p.x * inv_temp + (double)logf(p.y)) : -INFINITY; }
+__device__ inline float lse_of(float2 p, double inv_temp) { return p.y > 0.f ? (float)((double)p.x * inv_temp + (double)logf(p.y)) : -INFINITY; }
 
 struct TopArgs {
     const void* in;
     long long stride;
     int V, k, segs, seg_len, slots;   // slots: places for the candidates of a segment, k or more
-    float inv_temp, c2;  // c2: logit -> base-2 exponent
+    double inv_temp;
+    float c2;            // logit -> base-2 exponent
     float* values;
     int32_t* ids;
     float* lse;          // may be null
@@ -554,7 +555,7 @@ extern "C" int psd_top_logits(const void* logits, int32_t dtype, int32_t n_rows,
     if (workspace_bytes < psd_top_logits_workspace_bytes(n_rows, vocab, k))
         PSD_FAIL(PSD_ENOMEM, err, "%s: workspace %zu < %zu bytes", who, workspace_bytes, psd_top_logits_workspace_bytes(n_rows, vocab, k));
     const int segs = top_segs(n_rows, vocab, k), blocks = (vocab + kTopBlock - 1) / kTopBlock;
-    TopArgs a{logits, stride, vocab, k, segs, (blocks + segs - 1) / segs * kTopBlock, segs > 1 ? top_slots(k) : 0, 1.f / temperature, kLog2e / temperature, values, ids, lse, nullptr, nullptr};
+    TopArgs a{logits, stride, vocab, k, segs, (blocks + segs - 1) / segs * kTopBlock, segs > 1 ? top_slots(k) : 0, 1.0 / (double)temperature, kLog2e / temperature, values, ids, lse, nullptr, nullptr};
     if (segs > 1) {
         a.lists = (u64*)workspace;
         a.parts = (float2*)((char*)workspace + align16((size_t)n_rows * segs * top_slots(k) * sizeof(u64)));

@@ -392,6 +392,14 @@ def test_top_ties_orders_and_short_rows(V, k, reps):
     check_top(check, k, 1.0, (values[:9], ids[:9], lse[:9]))
 
 
+@pytest.mark.parametrize("T", [0.7, 3.0, 0.013, 1.0])
+def test_top_lse_of_one_entry_is_its_quotient_rounded_once(T):
+    z = np.random.default_rng(1).normal(0, 300, (500, 1)).astype(np.float32)
+    _, _, lse = run_top(Rows(z, psd.F32), 500, 1, 1, T, psd.F32)
+    want = z[:, 0].astype(np.float64) / float(np.float32(T))
+    assert (np.abs(lse - want) <= U * np.abs(want) * (1 + 2.0 ** -20)).all()
+
+
 # ---- distilling ----------------------------------------------------------------------------------------
 
 def run_distill(x, n, V, values, ids, lse, k, T, div, weights, dtype, stride=None, want_grad=True, in_place=False, gstride=None, stream=None):
