@@ -173,11 +173,13 @@ def _dev_ptr(a):
     """Address of a device buffer; host arrays and tensors in host memory are refused (a kernel must not be given their addresses)."""
     if a is None:
         return None
-    if not hasattr(a, "data_ptr"):
-        raise TypeError(f"a device buffer (an object with data_ptr()) is needed, not {type(a).__name__}")
-    if not getattr(a, "is_cuda", True):
-        raise TypeError(f"a device buffer is needed, not a {type(a).__name__} in host memory")
-    return a.data_ptr() or None
+    try:
+        p = a.data_ptr()
+    except AttributeError:
+        raise TypeError(f"a device buffer (an object with data_ptr()) is needed, not {type(a).__name__}") from None
+    if getattr(a, "is_cuda", True):
+        return p or None
+    raise TypeError(f"a device buffer is needed, not a {type(a).__name__} in host memory")
 
 
 class DeviceBuffer:
