@@ -314,8 +314,8 @@ int psd_sample(const float* logits, int32_t n_rows, int32_t vocab, float tempera
 /* ---- Rows of logits around the stages: adjusting, recording, distilling --------------------------------------
  * Three operators on rows of logits.  All pointers are DEVICE memory of the current device; the calls only enqueue work on
  * `stream` (a hipStream_t passed as void*, NULL = the default stream), allocate nothing and may be captured into a graph.
- *   - dtype: PSD_F32 or PSD_BF16, the type of the logits (and of what is written in their shape); arithmetic is fp32 or wider and
- *     rounded once.  Rows start `stride` elements apart (>= vocab) and need the alignment of one element only; what lies between
+ *   - dtype: PSD_F32 or PSD_BF16, the type of the logits (and of what is written in their shape); arithmetic is fp32 or wider, and its
+ *     result is rounded once to that type.  Rows start `stride` elements apart (>= vocab) and need the alignment of one element only; what lies between
  *     the end of a row and the next one is neither read nor written.  1 <= rows of a call <= 65535.
  *   - Logits are finite or -inf; an entry of -inf has probability 0.  A temperature is finite, above 0, and so is 1.45 over it.
  *   - What a call writes (its workspace included) shares no memory with what it reads, but for the rows where that is said below.
@@ -366,7 +366,9 @@ int psd_adjust_logits(const void* logits, void* out, int32_t dtype, int32_t n_se
  * ln sum_v exp(z_v / temperature): top log-probabilities (value / temperature - lse), or what psd_distill reads of a teacher.
  *   values [n_rows][k] floats (the logits), ids [n_rows][k], lse [n_rows] (may be NULL)
  * Where a row has fewer than k entries above -inf, the places behind them hold -inf and token -1 (lse of a row without any: -inf).
- * 1 <= k <= PSD_MAX_TOP, k <= vocab.  workspace: psd_top_logits_workspace_bytes(n_rows, vocab, k) bytes, 16-byte aligned.
+ * lse is a float: probabilities taken from it are off by |lse| 2^-24 of themselves, so that rows far from 0 are better shifted towards it first.
+ * 1 <= k <= PSD_MAX_TOP, k <= vocab.  workspace: psd_top_logits_workspace_bytes(n_rows, vocab, k) bytes, 16-byte aligned
+ * (few rows may need more than many do: their parts are merged).
  * Errors: PSD_EINVAL, PSD_ENOMEM (workspace too small), PSD_EHIP. */
 #define PSD_MAX_TOP 256
 size_t psd_top_logits_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t k);
@@ -386,11 +388,14 @@ int psd_top_logits(const void* logits, int32_t dtype, int32_t n_rows, int32_t vo
  *   complete or S the whole vocabulary; q_rest = the student's mass outside S.  Where the student has no mass outside S (its entries there are
  *   -inf, or each below 2^-126 of its largest entry's), a p_rest up to (2 + |lse|) 2^-22 is taken for the rounding of a record that
  *   holds all of the teacher's entries, and counts as 0.
- *   PSD_DIV_KL   sum p ln(p / q)          PSD_DIV_JSD   Div of this library on these outcomes: never above Div of the whole rows
+ *   PSD_DIV_KL   sum p ln(p / q)          PSD_DIV_JSD   Div of this library on these outcomes: with lse, and but for
+ *                                                 roundings, never above Div of the whole rows
  *   loss[r] = row_weights[r] * divergence,  grad[r][v] = d loss[r] / d z[r][v]
  * row_weights NULL: 1 everywhere.  A row of weight 0 (padding), or without a valid place, has loss 0 and gradient 0; its student row
- * is not looked at.  KL is +inf where the student has no mass that fp32 holds for an outcome of the teacher; a student row without any entry
- * above -inf, or a record without top_lse that has places but no value above -inf, has loss and gradient NaN.  row_weights is also where a gradient with respect to the losses goes: a second call then yields the product.
+ * is not looked at.  KL is +inf where an outcome of p > 0 meets student entries of -inf, or ones whose distance from the student's largest entry,
+ * times 1.4427 / temperature, is no float; a student's probability that merely underflows has its finite logarithm.  A student row without any
+ * entry above -inf, or a record without top_lse that has places but no value above -inf, has loss and gradient NaN.  row_weights is also
+ * where a gradient with respect to the losses goes: a second call then yields the product.
  *   top_values, top_ids [n_rows][k], 1 <= k <= PSD_MAX_TOP; top_lse, row_weights, loss [n_rows]
  *   grad: rows as the logits', of their type, grad_stride apart; NULL: the loss alone.  It may be `logits` itself (with equal
  *   strides); other overlaps are refused.

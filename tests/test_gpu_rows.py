@@ -700,6 +700,30 @@ def test_distill_a_whole_record_without_an_entry_is_no_distribution(n, V, div):
     assert only.tobytes() == loss.tobytes()
 
 
+@pytest.mark.parametrize("div", [psd.DIV_KL, psd.DIV_JSD])
+def test_distill_student_logits_far_below_the_rest(div):
+    """A student's logit whose probability fp32 does not hold has a finite logarithm, and so a finite divergence."""
+    rng = np.random.default_rng(12)
+    V = 3000
+    z = rng.normal(0, 1, (4, V)).astype(np.float32)
+    values, ids = np.tile(np.array([2.0, 1.0, 0.5], np.float32), (4, 1)), np.tile(np.array([5, 9, 2999], np.int32), (4, 1))
+    lse = np.full(4, 3.0, np.float32)
+    z[0, 5] = -1000.0                               # one of them
+    z[1, [5, 9, 2999]] = -1000.0                    # all of them
+    z[2] = -1000.0                                  # all but them
+    z[2, [5, 9, 2999]] = 1.0
+    z[3, 9] = -3.402823466e38                       # the difference, scaled, is no float
+    loss, grad = run_distill(Rows(z, psd.F32), 4, V, values, ids, lse, 3, 1.0, div, None, psd.F32)
+    for r in range(3):
+        want, wg, tol, gtol = distill_bounds(z[r], values[r], ids[r], lse[r], 1.0, div, 1.0)
+        # sum p ln q, where ln q is 1000 and its argument three roundings (sum p |ln p| is below 5)
+        tol += 3 * U * (abs(want) + 5)
+        assert abs(loss[r] - want) <= tol, (r, loss[r], want, tol)
+        assert (np.abs(grad[r] - wg) <= gtol + 1e-38).all()
+    assert np.isposinf(loss[3]) if div == psd.DIV_KL else 0 < loss[3] < np.log(2)
+    assert np.isfinite(grad).all()
+
+
 def test_distill_gradient_is_that_of_differences_of_its_own_loss():
     rng = np.random.default_rng(8)
     V, k, T = 300, 9, 1.0
