@@ -45,7 +45,6 @@ struct TopLds {
     };
     float2 part[kTopThreads / 64];
     alignas(16) uint4 least[kTopThreads / 64];
-    u64 smallest[kTopThreads / 64];
     int count;
 };
 
