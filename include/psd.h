@@ -335,7 +335,7 @@ int psd_sample(const float* logits, int32_t n_rows, int32_t vocab, float tempera
  *                    them; they are brought into 0 .. n_history, and an end before its beginning means none)
  *   n_prompt         [n_seqs]
  *   window           [n_seqs][window_stride], the first rows - 1 of each used; window_stride >= rows - 1
- *   penalties        [n_seqs][3]: repetition, presence, frequency; a repetition that is not above 0 counts as 1
+ *   penalties        [n_seqs][3], finite: repetition, presence, frequency; a repetition that is not above 0 counts as 1
  *   bias_tokens, bias  lists of all sequences, bias_offsets as history_offsets with n_bias (<= 2^30)
  *   masks            [n_masks][(vocab + 31) / 32] words, bit v % 32 of word v / 32 set: token v is allowed (a grammar's states, say)
  *   mask_index       [n_seqs * rows]: the mask of a row, -1 for none; for any other number outside 0 .. n_masks - 1 nothing is allowed

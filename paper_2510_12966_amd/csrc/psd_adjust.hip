@@ -6,7 +6,7 @@
 // window after each.
 // Bound: the bytes of the rows, read once and written once: 4.8 TB/s with 2000 tokens of history and 9 fp32 rows of 128255 for each of 48
 // sequences (93 us), as a large copy has.  Long histories: every chunk's workgroups go through all of it, out of their die's L2; 64 bf16 rows
-// with 30000 tokens each (15000 to 45000) take 17 us, 8 of them without any history.  Few rows: one launch and three loads that wait for
+// with 30000 tokens each (15000 to 45000) take 17 us, 10 without any history.  bf16 rows have twice the entries per byte: 432 of 128256, 55 us, 4.1 TB/s.  Few rows: one launch and three loads that wait for
 // one another (where the lists lie, their tokens, what they count), 4.9 us for one row.
 #include "psd_rows.h"
 
@@ -353,7 +353,9 @@ extern "C" int psd_adjust_logits(const void* logits, void* out, int32_t dtype, i
     if (!a.penalties) a.history = nullptr, a.window = nullptr;
     g.counts = a.history || a.window;
     g.biases = a.bias != nullptr;
-    // Chunks of 4096 entries (a workgroup of 256 threads, five a unit), or of 16384 (512 threads, two a unit): every chunk goes through all of
+    // Chunks of 4096 entries (a workgroup of 256 threads, four a unit with fp32 rows, five with bf16), or of 16384 (512 threads, two a unit; one where all
+    // lists of biases together pass some 3500 entries, since the room in LDS is for them all: 64 bf16 rows with 30000 tokens, 40 / 60 biases
+    // each 16.6 / 24.4 us): every chunk goes through all of
     // its sequence's history, so longer histories take larger chunks, the sooner the fuller the chip is without (us, 4096 / 16384; one row of 128256
     // for each sequence, fp32: 1 sequence with 12000 tokens 7.5 / 8.8, 30000: 11.0 / 11.1; 32 with 3000 8.8 / 9.8, 12000: 12.7 / 11.1; 64 with 500
     // 15.2 / 12.1, 30000: 37.8 / 18.7; 9 rows for each of 64: 500 tokens 114.5 / 117.5, 30000: 129.4 / 122.4)

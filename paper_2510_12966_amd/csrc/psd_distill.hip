@@ -14,7 +14,9 @@
 // them padding, 348 us) against 4.7 of a large copy.  The loss alone of 777 bf16 rows of 50257 takes 22.7 us, 3.1 TB/s: an exponential and five
 // more instructions per entry take about as long as the reads, and three workgroups a unit do not hide one behind the other altogether (two groups
 // of vectors on their way, in registers that take turns: 25.2 us).
-// Exponentials and logarithms are fp32, differences, sums and coefficients 64 bits.
+// The sums of the student's exponentials are fp32 (no entry passes through more than V / 256 + 96 additions), and so are
+// its scaled differences, the record's p and the shares of JSD; the record's sums, the two log-sum-exps' logarithms, the losses and the coefficients are
+// 64 bits.  Against 64 bits throughout: 1.5e-7 of the outputs' size, fp32, for the cases of perf/operators.py.
 #include "psd_rows.h"
 
 namespace psd {
@@ -311,7 +313,8 @@ __device__ inline float2 wave_tail(float m, float s, const raw16& mine, float c2
 // ---- one workgroup per row, which holds it --------------------------------------------------------------
 // A thread has HELD 16-byte vectors t, t + NT, t + 2 NT ... of the row, LDS of them in LDS and the others in registers, so that 512
 // threads of 256 registers and 144 KB of LDS hold 504 KB, all but all of a compute unit.  Shorter rows take fewer threads or registers,
-// and two or three workgroups share the unit, one reading while another computes or writes.  A vector with tokens of the record is left
+// and two or three workgroups share the unit, one reading while another computes or writes.  Besides the vectors a few values of the phases between
+// do not fit: the compiler keeps 22 registers of <256, 32> in scratch memory and 4 of <256, 63> and of the fp32 <512, 63>.  A vector with tokens of the record is left
 // out of the sums and of the stores (a bit per vector, a word per thread): the thread of its first place takes the vector's other elements
 // and writes all of it.  The row's last, incomplete vector is the business of thread k (which has no place) in the same way.
 template <bool BF16, int NT, int HELD, int LDS, int WAVES>
@@ -774,9 +777,12 @@ __global__ __launch_bounds__(kDisThreads) void distill_grad(const DistillArgs a)
 // one of 256 threads with 32 or 63 vectors each or of 512 with 63.  The loss takes the same sums in the same order with a gradient or without.
 //   chunks   few long rows, which leave most units idle otherwise: 12 MB of them, 20 MB where a row has 256 KB (us, chunks / passing; 65536 fp32
 //            entries: 64 rows 12.9 / 13.8, 89 rows 14.9 / 14.1; 128256: 29 rows 17.2 / 21.7, 48 rows 22.9 / 22.0; bf16: 64 rows 16.3 / 19.5, 89 rows
-//            21.3 / 19.7; 65536 bf16: 64 rows 12.0 / 12.7, 108 rows 15.3 / 13.2), and rows over 1 MB
+//            21.3 / 19.7; 65536 bf16: 64 rows 12.0 / 12.7, 108 rows 15.3 / 13.2; 49152 bf16: 32 rows 10.4 / 11.9, 100 rows 12.7 / 12.2; the loss alone
+//            of 4 / 64 such rows 10.3 / 8.9 and 10.0 / 10.2), and rows over 1 MB
 //   holding  rows from 96 KB, 240 MB of them in all: there the second pass comes from memory (passing / holding; 128256 fp32 entries: 800 rows
-//            195 / 178, 300 rows 76 / 73; bf16: 2000 rows 238 / 205, 800 rows 97 / 100; 50257 bf16: 3000 rows 196 / 170, 1200 rows 72 / 79)
+//            195 / 178, 300 rows, which pass, 76 / 73; bf16: 2000 rows 238 / 205, 800 rows 97 / 100; 50257 bf16: 3000 rows 196 / 170, 1200 rows 72 / 79).
+//            Rows beyond 504 KB pass all the same (1024 rows of 129024 fp32 entries, held: 204, of 131072: 286), and with k = 256, where thread k of 256 has
+//            a place, 512 threads hold a row (4096 bf16 rows of 128256, JSD: 422 with k = 255, 600)
 //   passing  1024 threads for at most a row per unit, 512 for rows over 128 KB (65536 fp32 entries, 2000 rows: 237, with 256 threads 291), else 256
 //            (50257 bf16, 800 rows: 55, with 512 threads 59; 4000 fp32 entries, 1000 rows: 11.7, with 1024 threads 25.5)
 enum Way { PASS_256, PASS_512, PASS_1024, HOLD_128K, HOLD_252K, HOLD_504K, CHUNKS };
