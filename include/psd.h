@@ -315,8 +315,8 @@ int psd_sample(const float* logits, int32_t n_rows, int32_t vocab, float tempera
  * Three operators on rows of logits.  All pointers are DEVICE memory of the current device; the calls only enqueue work on
  * `stream` (a hipStream_t passed as void*, NULL = the default stream), allocate nothing and may be captured into a graph.
  *   - dtype: PSD_F32 or PSD_BF16, the type of the logits (and of what is written in their shape); arithmetic is fp32 or wider, and its
- *     result is rounded once to that type.  Rows start `stride` elements apart (>= vocab) and need the alignment of one element only; what lies between
- *     the end of a row and the next one is neither read nor written.  1 <= rows of a call <= 65535.
+ *     result is rounded once to that type.  Rows start `stride` elements apart (>= vocab) and need the alignment of one element only;
+ *     what lies between the end of a row and the next one is neither read nor written.  1 <= rows of a call <= 65535.
  *   - Logits are finite or -inf; an entry of -inf has probability 0.  A temperature is finite, above 0, and so is 1.45 over it.
  *   - What a call writes (its workspace included) shares no memory with what it reads, but for the rows where that is said below.
  *   - A workspace belongs to one call until its kernels are done: calls (or captured graphs) that may overlap need one each.  Nothing in

@@ -5,9 +5,10 @@
 // counts do not depend on their order), and then goes through its rows, the next one on its way while one is written, adding one token of the
 // window after each.
 // Bound: the bytes of the rows, read once and written once: 4.8 TB/s with 2000 tokens of history and 9 fp32 rows of 128255 for each of 48
-// sequences (93 us), as a large copy has.  Long histories: every chunk's workgroups go through all of it, out of their die's L2; 64 bf16 rows
-// with 30000 tokens each (15000 to 45000) take 17 us, 10 without any history.  bf16 rows have twice the entries per byte: 432 of 128256, 55 us, 4.1 TB/s.  Few rows: one launch and three loads that wait for
-// one another (where the lists lie, their tokens, what they count), 4.9 us for one row.
+// sequences (93 us), as a large copy has; bf16 rows have twice the entries per byte: 432 of 128256, 55 us, 4.1 TB/s.  Long histories: every
+// chunk's workgroups go through all of it, out of their die's L2; 64 bf16 rows with 30000 tokens each (15000 to 45000) take 17 us, 10 without
+// any history.  Few rows: one launch and three loads that wait for one another (where the lists lie, their tokens, what they count), 4.9 us for
+// one row.
 #include "psd_rows.h"
 
 #include <algorithm>

@@ -313,9 +313,9 @@ __device__ inline float2 wave_tail(float m, float s, const raw16& mine, float c2
 // ---- one workgroup per row, which holds it --------------------------------------------------------------
 // A thread has HELD 16-byte vectors t, t + NT, t + 2 NT ... of the row, LDS of them in LDS and the others in registers, so that 512
 // threads of 256 registers and 144 KB of LDS hold 504 KB, all but all of a compute unit.  Shorter rows take fewer threads or registers,
-// and two or three workgroups share the unit, one reading while another computes or writes.  Besides the vectors a few values of the phases between
-// do not fit: the compiler keeps 22 registers of <256, 32> in scratch memory and 4 of <256, 63> and of the fp32 <512, 63>.  A vector with tokens of the record is left
-// out of the sums and of the stores (a bit per vector, a word per thread): the thread of its first place takes the vector's other elements
+// and two or three workgroups share the unit, one reading while another computes or writes.  Besides the vectors a few values of the phases
+// between do not fit: the compiler keeps 22 registers of <256, 32> in scratch memory and 4 of <256, 63> and of the fp32 <512, 63>.  A
+// vector with tokens of the record is left out of the sums and of the stores (a bit per vector, a word per thread): the thread of its first place takes the vector's other elements
 // and writes all of it.  The row's last, incomplete vector is the business of thread k (which has no place) in the same way.
 template <bool BF16, int NT, int HELD, int LDS, int WAVES>
 __global__ __launch_bounds__(NT, WAVES) void distill_row(const DistillArgs a) {
